@@ -69,6 +69,10 @@ typedef enum { QM_ROUND_RTNE = 0, QM_ROUND_STOCHASTIC_L = 1, QM_ROUND_STOCHASTIC
  *  FP32:         fp32 multiply-add on the CUDA cores (fp32 or bf16 operands). */
 typedef enum { QM_REF_BF16_FP32ACC = 0, QM_REF_FP32 = 1 } qm_ref;
 
+/* Activations of qm_gated_linear_int8: x / (1 + exp(-x)); x/2 (1 + erf(x / sqrt 2)); and the latter with
+ * the normal law's integral taken as 1/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))). */
+typedef enum { QM_ACT_SILU = 0, QM_ACT_GELU = 1, QM_ACT_GELU_TANH = 2 } qm_act;
+
 typedef struct {
   const void* data;        /* device; 16-byte aligned                                     */
   int32_t dtype;           /* qm_dtype                                                    */
@@ -274,6 +278,60 @@ qm_status qm_gemm(const uint8_t* codes_l, int32_t fmt_l, const float* delta_l, i
  */
 qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t N, int64_t K,
                       int64_t batch, float* out, void* stream);
+
+/*
+ * The operators of a layer whose projections run in 8 bits, for use with the formats that the probe
+ * has found good enough: a norm that leaves codes, and the INT8 product of codes, plain and gated.
+ * (The paper's layers quantize what a norm has written and descale into fp32; these
+ * calls do the same arithmetic without the tensors in between.)  All three take matrices of any extents and
+ * any row pitch; rows that are multiples of 16 bytes, 16-byte aligned, are the fast case.  M or rows may
+ * be 0: nothing is done then, and pointers are not looked at.
+ *
+ * qm_rms_norm_quantize, per row of `cols` elements:
+ *   z = x + residual, rounded to the stream's type (fp32, or bf16 to nearest even)
+ *   v = z * weight in fp32;  d = max|v| / qmax;  codes = sat(RTNE(v / d)), as qm_quantize(v) gives them
+ *   delta = d / sqrt(mean(z^2) + eps)
+ * so that code * delta stands for z * weight / rms(z): the norm's factor is one positive number for the
+ * row and cancels in Eq. 1's quotient, so the codes do not depend on how the squares were summed (fp32).
+ *  x, residual, residual_out   bf16 or fp32 (`dtype`), rows ld_* elements apart.  residual and residual_out are
+ *             both NULL (z = x) or both given; residual_out receives z and may be x or residual itself
+ *             (same pointer, same pitch), no other overlap.
+ *  weight     `cols` values, bf16 or fp32 (`weight_dtype`).
+ *  eps        positive and normal in fp32.
+ *  codes      [rows][qm_code_ld(cols)], 16-byte aligned, padding zero;  delta [rows] fp32.
+ * A row whose v is all zero gets delta = 1.  A NaN or Inf in x, residual or (where z is not zero) the products, or a sum
+ * of squares beyond fp32, makes the row's delta NaN and its codes 0; other rows are as they would be without it.
+ */
+qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int32_t dtype,
+                               const void* weight, int32_t weight_dtype, float eps, int64_t rows, int64_t cols,
+                               int32_t fmt, void* residual_out, int64_t ld_out, uint8_t* codes, float* delta,
+                               void* stream);
+
+/*
+ * qm_linear_int8: y_ij = (sum_k x_ik w_jk) * (delta_x[i] * delta_w[j]) + bias[j], the sum in int32 (exact; K up to
+ * 131071, codes of -128 included), the rest in fp32, rounded once to the output's type.
+ *  codes_x    [M] rows of K INT8 codes, ld_x bytes apart;  delta_x [M], a scale per row (token)
+ *  codes_w    [N] rows of K codes, ld_w bytes apart;        delta_w [N], a scale per output channel
+ *             (both 16-byte aligned, pitches multiples of 16, e.g. qm_code_ld(K); bytes from K on are not looked at)
+ *  bias       optional (NULL), N values of bias_dtype (qm_dtype)
+ *  out        [M] rows of N values of out_dtype (qm_dtype), ld_out elements apart; what lies between the rows stays
+ * A NaN scale gives NaN in its row or column.  Results do not depend on M or on how the work is split.
+ * A wait inside the kernel that runs into its time limit leaves NaN in the outputs it could not compute.
+ */
+qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_w, int64_t ld_w,
+                         const float* delta_w, const void* bias, int32_t bias_dtype, int64_t M, int64_t N, int64_t K,
+                         void* out, int32_t out_dtype, int64_t ld_out, void* stream);
+
+/*
+ * qm_gated_linear_int8: h = act(g) * u with g = x . gate^T and u = x . up^T as in qm_linear_int8 (no bias), both
+ * products, the activation (qm_act) and the multiplication in one kernel; g and u are not written.  codes_gate and codes_up may be
+ * two halves of one tensor.  act(g) is evaluated in fp32; where g is so negative that act(g) is below fp32's
+ * range, h is 0 (of either sign).  Other arguments as for qm_linear_int8.
+ */
+qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_gate,
+                               int64_t ld_gate, const float* delta_gate, const uint8_t* codes_up, int64_t ld_up,
+                               const float* delta_up, int32_t act, int64_t M, int64_t N, int64_t K, void* out,
+                               int32_t out_dtype, int64_t ld_out, void* stream);
 
 /*
  * Eq. 3 on materialised arrays: ref = C, q = Q, den = D, each `count` fp32

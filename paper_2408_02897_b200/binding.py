@@ -3,6 +3,7 @@
 Tensors are torch CUDA tensors (torch is used for device memory and streams); an operand of a
 product L.R is described by `operand_of(tensor, contract_dim)`.
 """
+import contextlib
 import ctypes as C
 import os
 import threading
@@ -15,6 +16,7 @@ _LIB_PATH = os.path.join(_HERE, "libqm.so")
 FMT = {"int8": 0, "e4m3": 1, "e5m2": 2}
 GRAN = {"tensor": 0, "channel": 1}
 REF = {"bf16": 0, "fp32": 1}
+ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 _DT = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -104,6 +106,9 @@ def lib():
             "qm_quantize_formats": (I32, [OP, I32, C.POINTER(I32), I32, C.POINTER(P), C.POINTER(P), P, P, P]),
             "qm_gemm": (I32, [P, I32, P, I32, P, I32, P, I32, I64, I64, I64, I64, P, P, I32, P]),
             "qm_gemm_ref": (I32, [P, P, I64, I64, I64, I64, P, P]),
+            "qm_rms_norm_quantize": (I32, [P, I64, P, I64, I32, P, I32, C.c_float, I64, I64, I32, P, I64, P, P, P]),
+            "qm_linear_int8": (I32, [P, I64, P, P, I64, P, P, I32, I64, I64, I64, P, I32, I64, P]),
+            "qm_gated_linear_int8": (I32, [P, I64, P, P, I64, P, P, I64, P, I32, I64, I64, I64, P, I32, I64, P]),
             "qm_metric_workspace_bytes": (SZ, [I64]),
             "qm_metric": (I32, [P, P, P, I64, P, P, SZ, P]),
             "qm_metric_scalars": (I32, [C.POINTER(MetricResult), C.POINTER(MetricScalars)]),
@@ -258,6 +263,132 @@ def qm_gemm_ref(l, r, stream=None):
     assert l.is_contiguous() and r.is_contiguous() and l.dtype == torch.bfloat16 and r.dtype == torch.bfloat16
     out = torch.empty((b, M, N), dtype=torch.float32, device="cuda")
     _check(lib().qm_gemm_ref(_ptr(l), _ptr(r), M, N, K, b, _ptr(out), _stream(stream)), "qm_gemm_ref")
+    return out
+
+
+def _refuse(why):
+    raise QmError(1, why)
+
+
+def _matrix(t, what, dtypes, device):
+    """(rows, cols, pitch) of a 2-D tensor, or a 3-D one with one batch element, whose rows are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3 and shape[0] == 1:
+        shape, stride = shape[1:], stride[1:]
+    if len(shape) != 2 or t.dtype not in dtypes or t.get_device() != device:
+        _refuse(f"{what}: wants a 2-D {' or '.join(map(str, dtypes))} tensor on the current CUDA device")
+    rows, cols = shape
+    if stride[1] != 1 and cols > 1:
+        _refuse(f"{what}: the elements of a row must be contiguous")
+    return rows, cols, stride[0] if rows > 1 else cols
+
+
+def _vector(t, what, n, dtypes, device):
+    """Address of a contiguous tensor of n values."""
+    if t.dtype not in dtypes or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what}: wants {n} contiguous {' or '.join(map(str, dtypes))} values on the current CUDA device")
+    return t.data_ptr()
+
+
+def _on(stream):
+    """(device, stream handle, context to allocate in): new tensors belong to the stream that writes them."""
+    device = torch.cuda.current_device()
+    if stream is None:
+        return device, torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
+    if stream.device_index != device:
+        _refuse("the stream is not one of the current CUDA device")
+    return device, stream.cuda_stream, torch.cuda.stream(stream)
+
+
+_FLOATS, _FP32, _BYTES = (torch.bfloat16, torch.float32), (torch.float32,), (torch.uint8,)
+
+
+def qm_rms_norm_quantize(x, weight, eps, fmt, residual=None, residual_out=None, stream=None):
+    """RMS norm of x + residual in 8 bits, a scale per row (token): (codes [1, rows, qm_code_ld(cols)], delta [rows],
+    residual_out or None).  codes * delta stands for z * weight / rms(z), z = x + residual in x's type, which residual_out
+    receives (made here when none is passed; it may be x or residual itself).  x, residual and residual_out are [rows, cols]
+    with contiguous rows of any pitch; the codes and scales are what qm_gemm and qm_linear_int8 take."""
+    device, handle, alloc = _on(stream)
+    rows, cols, ld = _matrix(x, "x", _FLOATS, device)
+    dt = x.dtype
+    w = _vector(weight, "weight", cols, _FLOATS, device)
+    r = z = None
+    ld_r = ld_z = 0
+    with alloc:
+        codes = torch.empty((1, rows, qm_code_ld(cols)), dtype=torch.uint8, device=x.device)
+        delta = torch.empty(rows, dtype=torch.float32, device=x.device)
+        if residual is not None:
+            if residual_out is None:
+                residual_out = torch.empty((rows, cols), dtype=dt, device=x.device)
+            r_rows, r_cols, ld_r = _matrix(residual, "residual", (dt,), device)
+            z_rows, z_cols, ld_z = _matrix(residual_out, "residual_out", (dt,), device)
+            if not r_rows == z_rows == rows or not r_cols == z_cols == cols:
+                _refuse("x, residual and residual_out differ in shape")
+            r, z = residual.data_ptr(), residual_out.data_ptr()
+        elif residual_out is not None:
+            _refuse("residual_out without residual")
+    st = lib().qm_rms_norm_quantize(x.data_ptr(), ld, r, ld_r, _DT[dt], w, _DT[weight.dtype], eps, rows, cols, FMT[fmt], z, ld_z,
+                                    codes.data_ptr(), delta.data_ptr(), handle)
+    if st:
+        _check(st, "qm_rms_norm_quantize")
+    return codes, delta, residual_out
+
+
+def _codes(t, what, K, device):
+    rows, width, ld = _matrix(t, what, _BYTES, device)
+    if width < K:
+        _refuse(f"{what}: rows of {width} codes, K is {K}")
+    return rows, max(ld, qm_code_ld(K)) if rows <= 1 else ld
+
+
+def _linear_out(out, out_dtype, M, N, alloc, device):
+    if out is None:
+        if out_dtype not in _DT:
+            _refuse("out_dtype: torch.bfloat16 or torch.float32")
+        with alloc:
+            out = torch.empty((M, N), dtype=out_dtype, device=torch.device("cuda", device))
+        return out, N
+    rows, cols, ld = _matrix(out, "out", _FLOATS, device)
+    if rows != M or cols != N:
+        _refuse(f"out: wants [{M}, {N}]")
+    return out, ld
+
+
+def qm_linear_int8(codes_x, delta_x, codes_w, delta_w, K, bias=None, out_dtype=torch.bfloat16, out=None, stream=None):
+    """INT8 product with a scale per token and per output channel -> [M, N] in bf16 or fp32:
+    (codes_x . codes_w^T) * (delta_x outer delta_w) + bias.  codes_x [M, >= K] and codes_w [N, >= K] are rows of INT8 codes
+    (uint8 tensors, 2-D or with a leading 1, pitch a multiple of 16), as qm_rms_norm_quantize and qm_quantize(.., "channel")
+    leave them; `out` may be a view with any row pitch (its type then counts, not out_dtype)."""
+    device, handle, alloc = _on(stream)
+    M, ld_x = _codes(codes_x, "codes_x", K, device)
+    N, ld_w = _codes(codes_w, "codes_w", K, device)
+    dx, dw = _vector(delta_x, "delta_x", M, _FP32, device), _vector(delta_w, "delta_w", N, _FP32, device)
+    b = _vector(bias, "bias", N, _FLOATS, device) if bias is not None else None
+    out, ld = _linear_out(out, out_dtype, M, N, alloc, device)
+    st = lib().qm_linear_int8(codes_x.data_ptr(), ld_x, dx, codes_w.data_ptr(), ld_w, dw, b,
+                              _DT[bias.dtype] if b is not None else 0, M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
+    if st:
+        _check(st, "qm_linear_int8")
+    return out
+
+
+def qm_gated_linear_int8(codes_x, delta_x, codes_gate, delta_gate, codes_up, delta_up, K, act="silu", out_dtype=torch.bfloat16,
+                         out=None, stream=None):
+    """The gated form act(x . gate^T) * (x . up^T) of qm_linear_int8, one kernel, -> [M, N].  act: "silu", "gelu" or
+    "gelu_tanh".  codes_gate and codes_up [N, >= K] may be the halves of one tensor."""
+    device, handle, alloc = _on(stream)
+    M, ld_x = _codes(codes_x, "codes_x", K, device)
+    N, ld_g = _codes(codes_gate, "codes_gate", K, device)
+    N_up, ld_u = _codes(codes_up, "codes_up", K, device)
+    if N != N_up:
+        _refuse("codes_gate and codes_up differ in their number of rows")
+    dx = _vector(delta_x, "delta_x", M, _FP32, device)
+    dg, du = _vector(delta_gate, "delta_gate", N, _FP32, device), _vector(delta_up, "delta_up", N, _FP32, device)
+    out, ld = _linear_out(out, out_dtype, M, N, alloc, device)
+    st = lib().qm_gated_linear_int8(codes_x.data_ptr(), ld_x, dx, codes_gate.data_ptr(), ld_g, dg, codes_up.data_ptr(), ld_u, du,
+                                    ACT[act], M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
+    if st:
+        _check(st, "qm_gated_linear_int8")
     return out
 
 

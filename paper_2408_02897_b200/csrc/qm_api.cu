@@ -350,6 +350,104 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
   return launch_tc_gemm_ref(l_bf16, r_bf16, g, out, nullptr, static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+bool valid_dtype(int d) { return d == QM_DT_F32 || d == QM_DT_BF16; }
+uintptr_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+uintptr_t elem_bytes(int dtype) { return dtype == QM_DT_BF16 ? 2 : 4; }
+
+// Whether a tensor that is written leaves one that is read alone, or is that very tensor: element by element each place is
+// then read ahead of its own writing.  Rows of the same pitch may lie between one another.
+bool same_or_apart(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int64_t rows, int64_t cols, int64_t es) {
+  if (a == b && (ld_a == ld_b || rows == 1)) return true;
+  const uintptr_t a0 = addr(a), b0 = addr(b);
+  const uint64_t span_a = (uint64_t)((rows - 1) * ld_a + cols) * es, span_b = (uint64_t)((rows - 1) * ld_b + cols) * es;
+  if (a0 + span_a <= b0 || b0 + span_b <= a0) return true;
+  if (ld_a != ld_b || rows == 1) return false;
+  const uint64_t pitch = (uint64_t)ld_a * es, off = (a0 > b0 ? a0 - b0 : b0 - a0) % pitch, width = (uint64_t)cols * es;
+  return off >= width && pitch - off >= width;
+}
+
+// Extents and pitches whose products stay well inside 64 bits.
+bool sane(int64_t n) { return n < (1ll << 31); }
+bool sane_pitch(int64_t ld) { return ld < (1ll << 30); }
+}  // namespace
+
+qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int32_t dtype,
+                               const void* weight, int32_t weight_dtype, float eps, int64_t rows, int64_t cols,
+                               int32_t fmt, void* residual_out, int64_t ld_out, uint8_t* codes, float* delta,
+                               void* stream) {
+  if (!valid_dtype(dtype) || !valid_dtype(weight_dtype) || !valid_fmt(fmt) || rows < 0 || cols <= 0) return QM_ERR_INVALID_ARG;
+  if (!(eps >= 1.17549435e-38f && eps <= 3.402823466e38f)) return QM_ERR_INVALID_ARG;
+  if (rows == 0) return QM_OK;
+  if (!x || !weight || !codes || !delta || !residual != !residual_out) return QM_ERR_INVALID_ARG;
+  if (rows > 1 && (ld_x < cols || (residual && (ld_residual < cols || ld_out < cols)))) return QM_ERR_INVALID_ARG;
+  if (rows == 1) ld_x = ld_residual = ld_out = cols;
+  if (!sane(rows) || cols >= (1ll << 30) || !sane_pitch(ld_x) || (residual && (!sane_pitch(ld_residual) || !sane_pitch(ld_out))))
+    return QM_ERR_UNSUPPORTED;
+  const uintptr_t es = elem_bytes(dtype);
+  if (addr(x) % es || addr(residual) % es || addr(residual_out) % es || addr(weight) % elem_bytes(weight_dtype) ||
+      addr(codes) % 16 || addr(delta) % 4)
+    return QM_ERR_ALIGNMENT;
+  if (residual && (!same_or_apart(residual_out, ld_out, x, ld_x, rows, cols, es) ||
+                   !same_or_apart(residual_out, ld_out, residual, ld_residual, rows, cols, es)))
+    return QM_ERR_INVALID_ARG;
+  return launch_rms_norm({x, dtype, rows, cols, ld_x}, {residual, dtype, rows, cols, ld_residual}, residual_out, ld_out, weight,
+                         weight_dtype, eps, fmt, codes, delta, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+qm_status run_linear(LinearArgs a, cudaStream_t s) {
+  const bool gated = a.w[1] != nullptr;
+  if (!a.x || !a.dx || !a.w[0] || !a.dw[0] || (gated && !a.dw[1]) || !a.out) return QM_ERR_INVALID_ARG;
+  for (int p = 0; p < (gated ? 2 : 1); ++p)
+    if (a.N > 1 && a.ld_w[p] < a.K) return QM_ERR_INVALID_ARG;
+  if (a.M > 1 && (a.ld_x < a.K || a.ld_out < a.N)) return QM_ERR_INVALID_ARG;
+  // the pitch of a single row carries no information: give it the dense value
+  if (a.M == 1) { a.ld_x = qm_code_ld(a.K); a.ld_out = a.N; }
+  if (a.N == 1) a.ld_w[0] = a.ld_w[1] = qm_code_ld(a.K);
+  if (!sane(a.M) || a.N >= (1ll << 30) || a.K > 131071 || !sane_pitch(a.ld_x) || !sane_pitch(a.ld_w[0]) || !sane_pitch(a.ld_w[1]) ||
+      !sane_pitch(a.ld_out))
+    return QM_ERR_UNSUPPORTED;
+  if (addr(a.x) % 16 || a.ld_x % 16 || addr(a.dx) % 4 || addr(a.out) % elem_bytes(a.out_dtype) ||
+      (a.bias && addr(a.bias) % elem_bytes(a.bias_dtype)))
+    return QM_ERR_ALIGNMENT;
+  for (int p = 0; p < (gated ? 2 : 1); ++p)
+    if (addr(a.w[p]) % 16 || a.ld_w[p] % 16 || addr(a.dw[p]) % 4) return QM_ERR_ALIGNMENT;
+  return launch_linear_int8(a, s);
+}
+}  // namespace
+
+qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_w, int64_t ld_w,
+                         const float* delta_w, const void* bias, int32_t bias_dtype, int64_t M, int64_t N, int64_t K,
+                         void* out, int32_t out_dtype, int64_t ld_out, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || !valid_dtype(out_dtype) || (bias && !valid_dtype(bias_dtype))) return QM_ERR_INVALID_ARG;
+  if (M == 0) return QM_OK;
+  LinearArgs a{};
+  a.x = codes_x; a.ld_x = ld_x; a.dx = delta_x;
+  a.w[0] = codes_w; a.ld_w[0] = ld_w; a.dw[0] = delta_w;
+  a.bias = bias; a.bias_dtype = bias_dtype;
+  a.M = M; a.N = N; a.K = K;
+  a.out = out; a.out_dtype = out_dtype; a.ld_out = ld_out;
+  return run_linear(a, static_cast<cudaStream_t>(stream));
+}
+
+qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_gate,
+                               int64_t ld_gate, const float* delta_gate, const uint8_t* codes_up, int64_t ld_up,
+                               const float* delta_up, int32_t act, int64_t M, int64_t N, int64_t K, void* out,
+                               int32_t out_dtype, int64_t ld_out, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || !valid_dtype(out_dtype)) return QM_ERR_INVALID_ARG;
+  if (act != QM_ACT_SILU && act != QM_ACT_GELU && act != QM_ACT_GELU_TANH) return QM_ERR_INVALID_ARG;
+  if (M == 0) return QM_OK;
+  if (!codes_up) return QM_ERR_INVALID_ARG;
+  LinearArgs a{};
+  a.x = codes_x; a.ld_x = ld_x; a.dx = delta_x;
+  a.w[0] = codes_gate; a.ld_w[0] = ld_gate; a.dw[0] = delta_gate;
+  a.w[1] = codes_up; a.ld_w[1] = ld_up; a.dw[1] = delta_up;
+  a.M = M; a.N = N; a.K = K; a.act = act;
+  a.out = out; a.out_dtype = out_dtype; a.ld_out = ld_out;
+  return run_linear(a, static_cast<cudaStream_t>(stream));
+}
+
 size_t qm_metric_workspace_bytes(int64_t count) {
   if (count <= 0) return 0;
   return align256(sizeof(double) * kPartialDoubles * (size_t)metric_blocks(count));

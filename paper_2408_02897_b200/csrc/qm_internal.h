@@ -147,6 +147,25 @@ qm_status launch_tensor_stats(const View& x, qm_tensor_stats_result* out, void* 
 qm_status launch_quantize_error(const View& x, int fmt, int gran, const float* delta,
                                 qm_quant_error_result* out, void* ws, cudaStream_t s);
 
+// ---- RMS norm with 8-bit output (rms_norm.cu) -------------------------------
+// Rows of `cols` contiguous elements, `ld` elements apart.
+struct RowsView { const void* data; int dtype; int64_t rows, cols, ld; };
+// residual.data null: nothing is added and residual_out is not written.
+qm_status launch_rms_norm(const RowsView& x, const RowsView& residual, void* residual_out, int64_t ld_out,
+                          const void* weight, int weight_dtype, float eps, int fmt, uint8_t* codes, float* delta,
+                          cudaStream_t s);
+
+// ---- INT8 products of a layer (linear_int8.cu) ------------------------------
+struct LinearArgs {
+  const uint8_t* x; int64_t ld_x; const float* dx;
+  const uint8_t* w[2]; int64_t ld_w[2]; const float* dw[2];     // w[1] null: one product, not the gated form
+  const void* bias; int bias_dtype;
+  int64_t M, N, K;
+  int act;
+  void* out; int out_dtype; int64_t ld_out;
+};
+qm_status launch_linear_int8(const LinearArgs& a, cudaStream_t s);
+
 // ---- metric (metric.cu) ----------------------------------------------------
 // One partial record per CTA: {sum_be, max_be, sum_diff2, sum_ref2, sum_den2} as doubles.
 constexpr int kPartialDoubles = 5;
