@@ -252,6 +252,7 @@ qm_status launch_tc_probes(const TcProbeArgs* ps, int n, cudaStream_t s);
 // per CTA (0xffffffff: off), so that the consumers' waits run out.
 void set_wait_limit_ns(uint64_t ns);
 void set_stop_after_kb(uint32_t kb);
+void wait_settings(uint64_t* limit_ns, uint32_t* stop_after_kb);    // as they are now, for a launch
 qm_status launch_tc_gemm_lp(const uint8_t* cl, int fmt_l, const float* dl, int gran_l,
                             const uint8_t* cr, int fmt_r, const float* dr, int gran_r,
                             GemmShape g, float* out_descaled, void* out_raw, uint32_t* err_word,
