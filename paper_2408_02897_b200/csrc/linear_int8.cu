@@ -1,79 +1,594 @@
 // The products of a layer whose codes are INT8 (qm_linear_int8, qm_gated_linear_int8):
 //   y_ij = (sum_k x_ik w_jk) dx_i dw_j + bias_j          the sum in int32, exact
 //   h_ij = act(g_ij) u_ij, g and u two such products     of the same x
-// written in bf16 or fp32.
+// written in bf16 or fp32.  Two kernels, both on tcgen05.mma kind::i8 with operands staged by TMA in 128-byte-swizzled blocks
+// 128 contraction entries deep; a tail of the contraction is what the tensor map fills with zeros.
+//   linear_few_kernel   few rows of x.  A CTA takes 128 rows of the WEIGHT as the MMA's M and up to 128 rows of x as its N,
+//                       so that a weight row is a lane of tensor memory and an output row is written by consecutive lanes.
+//                       The contraction is split over the CTAs of a cluster.
+//   linear_many_kernel  CTA pairs (cta_group::2) on tiles of 256 rows of x and 256 weight rows, two accumulator buffers.
+// Integer sums are the same in any order, so an output does not depend on the kernel or the split.
+//
+// Every mbarrier wait is bounded (Waiter): a CTA that gives up leaves NaN in the outputs it cannot compute, waits for what it has
+// in flight, frees tensor memory and returns.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "qm_internal.h"
+#include "tc_ptx.cuh"
 
 namespace qm {
 namespace {
 
-constexpr int kTile = 64, kChunk = 64;         // outputs per side of a block's tile, contraction entries per step
+constexpr int kBlock = 128;                               // rows of a staged block, and its contraction entries
+constexpr uint32_t kBlockBytes = kBlock * kBlock;         // 16 KB
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;             // TMA warp, MMA warp, epilogue
+
+struct Scales {
+  const float* dx;
+  const float* dw[2];
+  const void* bias; int bias_bf16;
+  int act;
+};
+struct Waits { uint64_t limit_ns; uint32_t stop_after; };
 
 // act(g) in fp32.  The tanh form is g / (1 + exp(-2 t)), t the tanh's argument: 1/2 (1 + tanh t) is that quotient, and
-// unlike 1 + tanhf(t) it keeps its relative precision where t is negative.
+// unlike 1 + tanh(t) it keeps its relative precision where t is negative.  Both sides of the quotient are scaled by
+// 2^-20, because the fast division takes denominators below 2^126; beyond exp's range the quotient is 0.
 __device__ __forceinline__ float activate(float g, int act) {
   if (act == QM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
   const float t = act == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
-  return g / (1.f + expf(-t));
+  return __fdividef(g * 9.5367432e-7f, fmaf(__expf(-t), 9.5367432e-7f, 9.5367432e-7f));
 }
 
-__device__ __forceinline__ int load4(const uint8_t* row, int k, int K) {
-  uint32_t v = 0;
-  for (int i = 0; i < 4; ++i) v |= (k + i < K ? (uint32_t)row[k + i] : 0u) << (8 * i);
-  return (int)v;
+__device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
+  if (!s.bias) return 0.f;
+  return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
+}
+
+__device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
+
+// ------------------------------------------------------------------ few rows
+struct FewArgs {
+  int64_t M, N;
+  int num_kb, tiles_m, split, nt, stages;    // nt: rows of x per tile, 16 .. 128
+  uint32_t idesc, tmem_cols;
+  Scales sc;
+  Waits waits;
+  void* out; int64_t ld;
+};
+constexpr int kFewStages = 12;
+constexpr int kMaxSplit = 8;
+struct SharedFew {
+  uint64_t full[kFewStages], empty[kFewStages], done, drain;
+  uint32_t tmem_base, abort_flag, issued, pad;
+  float dx[256];
+};
+
+__device__ __forceinline__ uint32_t lds_cluster(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
 }
 
 template <typename T, bool GATED>
-__global__ void __launch_bounds__(256) linear_tile(const LinearArgs a) {
-  pdl_prologue();
-  __shared__ int sx[kChunk / 4][kTile + 1], sw[GATED ? 2 : 1][kChunk / 4][kTile + 1];
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  int acc[GATED ? 2 : 1][4][4] = {};
-  for (int k0 = 0; k0 < a.K; k0 += kChunk) {
-    for (int i = threadIdx.x; i < kTile * kChunk / 4; i += 256) {
-      const int row = i / (kChunk / 4), c = i % (kChunk / 4);
-      sx[c][row] = m0 + row < a.M ? load4(a.x + (m0 + row) * a.ld_x, k0 + 4 * c, (int)a.K) : 0;
-#pragma unroll
-      for (int p = 0; p < (GATED ? 2 : 1); ++p)
-        sw[p][c][row] = n0 + row < a.N ? load4(a.w[p] + (n0 + row) * a.ld_w[p], k0 + 4 * c, (int)a.K) : 0;
+__global__ void __launch_bounds__(kThreads, 1)
+linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                  const __grid_constant__ CUtensorMap map_u, const FewArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  constexpr int kW = GATED ? 2 : 1;
+  const uint32_t stage_bytes = kW * kBlockBytes + (uint32_t)a.nt * kBlock;
+  SharedFew* sh = reinterpret_cast<SharedFew*>(tiles + (size_t)a.stages * stage_bytes);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split;
+  const int n0 = tile / a.tiles_m * kBlock, m0 = tile % a.tiles_m * a.nt;
+  const int kb0 = (int)((int64_t)a.num_kb * part / a.split), kb1 = (int)((int64_t)a.num_kb * (part + 1) / a.split);
+  const Waiter w{&sh->abort_flag, nullptr, a.waits.limit_ns};
+
+  if (warp == 0 && lane < 2 + (int)GATED) {
+    const CUtensorMap* maps[3] = {&map_x, &map_w, &map_u};
+    asm volatile("prefetch.tensormap [%0];" ::"l"(maps[lane]) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < a.stages; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1);
+      mbar_init(smem_u32(&sh->empty[s]), 1);
     }
+    mbar_init(smem_u32(&sh->done), 1);
+    mbar_init(smem_u32(&sh->drain), 1);
+    sh->abort_flag = 0; sh->issued = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(a.tmem_cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  pdl_prologue();
+  tc_fence_after();
+  const uint32_t tmem_base = sh->tmem_base;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t g = 0;
+      int s = 0;
+      uint32_t parity = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++g) {
+        if (g >= a.waits.stop_after) break;
+        if (g >= (uint32_t)a.stages && !w.wait(smem_u32(&sh->empty[s]), parity ^ 1u)) break;
+        const uint32_t bar = smem_u32(&sh->full[s]), base = smem_u32(tiles) + (uint32_t)s * stage_bytes;
+        mbar_expect_tx(bar, stage_bytes);
+        tma_load_2d_local(base, &map_w, bar, kb * kBlock, n0);
+        if (GATED) tma_load_2d_local(base + kBlockBytes, &map_u, bar, kb * kBlock, n0);
+        tma_load_2d_local(base + kW * kBlockBytes, &map_x, bar, kb * kBlock, m0);
+        if (++s == a.stages) { s = 0; parity ^= 1u; }
+      }
+      sh->issued = g;
+    }
+  } else if (warp == 1) {
+    const bool lead = elect_one();
+    int s = 0;
+    uint32_t parity = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!w.wait_warp(smem_u32(&sh->full[s]), parity)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t base = smem_u32(tiles) + (uint32_t)s * stage_bytes;
+      const uint64_t dx = smem_desc(base + kW * kBlockBytes, 128);
+      if (lead) {
+#pragma unroll
+        for (int p = 0; p < kW; ++p)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)             // 32 codes per instruction
+            mma_i8_one(tmem_base + (uint32_t)(p * a.nt), smem_desc(base + p * kBlockBytes, 128) + 2 * k, dx + 2 * k, a.idesc,
+                       k ? 1u : (uint32_t)(kb > kb0));
+        tc_commit_one(smem_u32(&sh->empty[s]));
+      }
+      if (++s == a.stages) { s = 0; parity ^= 1u; }
+    }
+    if (ok && lead) tc_commit_one(smem_u32(&sh->done));
+  }
+
+  // epilogue, warps 2..9: a warp may read the quarter warp % 4 of tensor memory's lanes; the two warps of a quarter take every
+  // other chunk of 16 columns (rows of x)
+  const int et = (int)threadIdx.x - 64, q = warp & 3, h = (warp - 2) >> 2;
+  const int live = (int)(a.M - m0 < a.nt ? a.M - m0 : a.nt);                 // rows of x in this tile
+  T* const out = static_cast<T*>(a.out);
+  if (warp >= 2) {
+    if (et < live) sh->dx[et] = a.sc.dx[m0 + et];
+    const bool ok = w.wait_warp(smem_u32(&sh->done), 0);
+    tc_fence_after();
+    asm volatile("bar.sync 1, 256;" ::: "memory");                            // dx is there, and every warp has waited
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
+    const int j = q * 32 + lane;
+    const int64_t n = (int64_t)n0 + j;
+    if (a.split == 1) {
+      const bool col = n < a.N;
+      const float dw = col ? a.sc.dw[0][n] : 0.f, du = GATED && col ? a.sc.dw[1][n] : 0.f, bias = !GATED && col ? load_bias(a.sc, n) : 0.f;
+      for (int c = h * 16; c < live; c += 32) {
+        uint32_t r[16], u[16];
+        if (ok) {
+          tmem_ld16(lane_addr + c, r);
+          if (GATED) tmem_ld16(lane_addr + a.nt + c, u);
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (col && c + i < live) {
+            const float dxv = sh->dx[c + i];
+            float y = (float)(int)r[i] * (dxv * dw);
+            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[i] * (dxv * du)) : y + bias;
+            out[(int64_t)(m0 + c + i) * a.ld + n] = (T)(ok ? y : nan_f());
+          }
+      }
+    } else {
+      // this CTA's share of the sums, [row of x][weight row], for the cluster: the ring is not in use any more
+      int* const sums = reinterpret_cast<int*>(tiles);
+      for (int c = h * 16; ok && c < live; c += 32) {
+#pragma unroll
+        for (int p = 0; p < kW; ++p) {
+          uint32_t r[16];
+          tmem_ld16(lane_addr + p * a.nt + c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (c + i < live) sums[(p * a.nt + c + i) * kBlock + j] = (int)r[i];
+        }
+      }
+    }
+  }
+  if (a.split > 1) {
     __syncthreads();
-    for (int c = 0; c < kChunk / 4; ++c)
+    cluster_sync();
+    if (warp >= 2) {
+      bool ok = true;
+      for (int p = 0; p < a.split; ++p) ok = ok && lds_cluster(map_to_cta(smem_u32(&sh->abort_flag), p)) == 0;
+      const int total = live * kBlock, share = ((total + a.split - 1) / a.split + 31) & ~31;
+      const int end = min(total, (part + 1) * share);
+      const int j = (part * share + et) & (kBlock - 1);                       // the same for all elements of a thread
+      const int64_t n = (int64_t)n0 + j;
+      if (n < a.N) {
+        const float dw = a.sc.dw[0][n], du = GATED ? a.sc.dw[1][n] : 0.f, bias = !GATED ? load_bias(a.sc, n) : 0.f;
+        const uint32_t mine = smem_u32(tiles);
+        for (int e = part * share + et; e < end; e += 256) {
+          int g = 0, u = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int p = 0; p < (GATED ? 2 : 1); ++p)
-            acc[p][i][j] = __dp4a(sx[c][ty + 16 * i], sw[p][c][tx + 16 * j], acc[p][i][j]);
+          for (int p = 0; p < kMaxSplit; ++p)
+            if (p < a.split) {
+              const uint32_t peer = map_to_cta(mine, p);
+              g += (int)lds_cluster(peer + 4 * e);
+              if (GATED) u += (int)lds_cluster(peer + 4 * (a.nt * kBlock + e));
+            }
+          const int i = e / kBlock;
+          const float dxv = sh->dx[i];
+          float y = (float)g * (dxv * dw);
+          y = GATED ? activate(y, a.sc.act) * ((float)u * (dxv * du)) : y + bias;
+          out[(int64_t)(m0 + i) * a.ld + n] = (T)(ok ? y : nan_f());
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (sh->abort_flag) {
+    // give-up path: loads and MMAs that nobody has waited for
+    if (threadIdx.x == 0) {
+      const uint32_t n = sh->issued, st = (uint32_t)a.stages;
+      for (uint32_t g = n > st ? n - st : 0u; g < n; ++g) {
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&sh->full[g % st]), (g / st) & 1) && global_timer_ns() - t0 < a.waits.limit_ns) {}
+      }
+    }
+    if (warp == 1) {
+      if (elect_one()) tc_commit_one(smem_u32(&sh->drain));
+      const uint64_t t0 = global_timer_ns();
+      while (!mbar_try_wait(smem_u32(&sh->drain), 0) && global_timer_ns() - t0 < a.waits.limit_ns) {}
+    }
     __syncthreads();
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= a.M || n >= a.N) continue;
-      float y = (float)acc[0][i][j] * (a.dx[m] * a.dw[0][n]);
-      if (GATED) y = activate(y, a.act) * ((float)acc[GATED ? 1 : 0][i][j] * (a.dx[m] * a.dw[1][n]));
-      else if (a.bias) y += a.bias_dtype == QM_DT_BF16 ? (float)static_cast<const __nv_bfloat16*>(a.bias)[n]
-                                                       : static_cast<const float*>(a.bias)[n];
-      static_cast<T*>(a.out)[m * a.ld_out + n] = (T)y;
+  if (a.split > 1) cluster_sync();              // the peers have read this CTA's sums
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ many rows
+struct ManyArgs {
+  int64_t M, N;
+  int num_kb, tiles_n, num_tiles;              // tiles of 256 rows of x and 256 weight rows (gated: 128 of each weight)
+  Scales sc;
+  Waits waits;
+  void* out; int64_t ld;
+  int vec;                                     // rows of the output start on 16 bytes
+};
+constexpr int kManyStages = 5;
+constexpr uint32_t kManyStageBytes = 2 * kBlockBytes;
+struct SharedMany {
+  uint64_t full[kManyStages], empty[kManyStages], tmem_full[2], tmem_empty[2], drain;
+  uint32_t tmem_base, abort_flag, issued, pad;
+  float dw[2][256], bias[2][256];
+  uint4 stage[kEpiWarps][32 * 8];              // 32 rows of 128 bytes of output per epilogue warp
+};
+
+// The warp's 32 rows x 128 bytes of output out of shared memory, whole lines per instruction (16-byte units permuted with the row:
+// conflict-free both ways); ragged chunks and rows that do not start on 16 bytes an element per lane.
+template <typename T>
+__device__ __forceinline__ void store_rows(const uint4* stage, int lane, T* out, int64_t ld, int rows, int cols, bool vec) {
+  constexpr int kCols = 128 / sizeof(T);
+  if (cols == kCols && vec) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = 4 * i + (lane >> 3), u = lane & 7;
+      if (row < rows) *reinterpret_cast<uint4*>(out + row * ld + u * (16 / sizeof(T))) = stage[row * 8 + (u ^ (row & 7))];
     }
+  } else {
+    const T* w = reinterpret_cast<const T*>(stage);
+    constexpr int kUnit = 16 / sizeof(T);
+    for (int row = 0; row < rows; ++row)
+#pragma unroll
+      for (int c = lane; c < kCols; c += 32)
+        if (c < cols) out[row * ld + c] = w[row * kCols + ((c / kUnit) ^ (row & 7)) * kUnit + c % kUnit];
+  }
+}
+
+template <typename T, bool GATED>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                   const __grid_constant__ CUtensorMap map_u, const ManyArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  SharedMany* sh = reinterpret_cast<SharedMany*>(tiles + (size_t)kManyStages * kManyStageBytes);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const Waiter w{&sh->abort_flag, nullptr, a.waits.limit_ns};
+  constexpr int kTileN = GATED ? 128 : 256;                                   // output columns of a tile
+
+  if (warp == 0 && lane < 2 + (int)GATED) {
+    const CUtensorMap* maps[3] = {&map_x, &map_w, &map_u};
+    asm volatile("prefetch.tensormap [%0];" ::"l"(maps[lane]) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kManyStages; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1);
+      mbar_init(smem_u32(&sh->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&sh->tmem_full[b]), 1);
+      mbar_init(smem_u32(&sh->tmem_empty[b]), 2 * kEpiWarps);
+    }
+    mbar_init(smem_u32(&sh->drain), 1);
+    sh->abort_flag = 0; sh->issued = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  pdl_prologue();
+  tc_fence_after();
+  const uint32_t tmem_base = sh->tmem_base;
+
+  if (warp == 0) {
+    // TMA producer (both CTAs): this CTA's 128 rows of x, and its half of the MMA's N: the tile's weight rows, or of the gated
+    // form the gate's rows in the leader and up's in its peer, so that accumulator columns j and 128 + j are output column j's
+    if (lane == 0) {
+      const CUtensorMap* const mw = GATED && rank ? &map_u : &map_w;
+      uint32_t g = 0;
+      int s = 0;
+      uint32_t parity = 0;
+      bool ok = true;
+      for (int t = pair; t < a.num_tiles && ok; t += num_pairs) {
+        const int tm = t / a.tiles_n;
+        const int r0 = tm * 256 + (int)rank * kBlock, c0 = (t - tm * a.tiles_n) * kTileN + (GATED ? 0 : (int)rank * kBlock);
+        for (int kb = 0; kb < a.num_kb; ++kb, ++g) {
+          if (g >= a.waits.stop_after || (g >= (uint32_t)kManyStages && !w.wait(smem_u32(&sh->empty[s]), parity ^ 1u))) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(smem_u32(&sh->full[s]), 2 * kManyStageBytes);
+          const uint32_t bar = map_to_cta(smem_u32(&sh->full[s]), 0), base = smem_u32(tiles) + (uint32_t)s * kManyStageBytes;
+          tma_load_2d(base, &map_x, bar, kb * kBlock, r0);
+          tma_load_2d(base + kBlockBytes, mw, bar, kb * kBlock, c0);
+          if (++s == kManyStages) { s = 0; parity ^= 1u; }
+        }
+      }
+      sh->issued = g;
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const bool lead = elect_one();
+      constexpr uint32_t idesc = make_idesc(2, 1, 1, 256, 256);               // s8 x s8 -> s32
+      uint32_t it = 0;
+      int s = 0;
+      uint32_t parity = 0;
+      bool ok = true;
+      for (int t = pair; t < a.num_tiles && ok; t += num_pairs, ++it) {
+        const uint32_t buf = it & 1;
+        if (it >= 2 && !w.wait_warp(smem_u32(&sh->tmem_empty[buf]), ((it >> 1) - 1) & 1)) break;
+        tc_fence_after();
+        for (int kb = 0; kb < a.num_kb; ++kb) {
+          if (!w.wait_warp(smem_u32(&sh->full[s]), parity)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t base = smem_u32(tiles) + (uint32_t)s * kManyStageBytes;
+          const uint64_t da = smem_desc(base, 128), db = smem_desc(base + kBlockBytes, 128);
+          if (lead) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_pair<kKindI8>(tmem_base + buf * 256, da + 2 * k, db + 2 * k, idesc, k ? 1u : (uint32_t)(kb > 0), true);
+            tc_commit_pair(smem_u32(&sh->empty[s]), true);
+          }
+          if (++s == kManyStages) { s = 0; parity ^= 1u; }
+        }
+        if (ok) tc_commit_pair(smem_u32(&sh->tmem_full[buf]), lead);
+      }
+    }
+  } else {
+    // epilogue, warps 2..9 of both CTAs: a row of x per lane; the two warps of a lane quarter take half of the columns each
+    const int q = warp & 3, h = (warp - 2) >> 2, et = (int)threadIdx.x - 64;
+    uint4* const stage = sh->stage[warp - 2];
+    T* const out = static_cast<T*>(a.out);
+    constexpr int kChunk = 128 / sizeof(T);
+    bool ok = true;
+    uint32_t it = 0;
+    for (int t = pair; t < a.num_tiles; t += num_pairs, ++it) {
+      const int tm = t / a.tiles_n;
+      const uint32_t buf = it & 1;
+      const int64_t c0 = (int64_t)(t - tm * a.tiles_n) * kTileN;
+      {
+        // column scales by accumulator column (gated: gate's, then up's)
+        const int64_t col = c0 + (GATED ? et & 127 : et);
+        const bool in = col < a.N;
+        sh->dw[buf][et] = !in ? 0.f : GATED && et >= 128 ? a.sc.dw[1][col] : a.sc.dw[0][col];
+        if (!GATED) sh->bias[buf][et] = in ? load_bias(a.sc, col) : 0.f;
+      }
+      const int64_t row0 = (int64_t)tm * 256 + rank * kBlock + q * 32, row = row0 + lane;
+      const int rows = (int)(a.M - row0 < 32 ? a.M - row0 : 32);             // <= 0: none
+      const float dxv = row < a.M ? a.sc.dx[row] : 0.f;
+      ok = ok && w.wait_warp(smem_u32(&sh->tmem_full[buf]), (it >> 1) & 1);
+      asm volatile("bar.sync 1, 256;" ::: "memory");                          // publishes the scales
+      tc_fence_after();
+      const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256;
+#pragma unroll 1
+      for (int c = h * (kTileN / 2); c < (h + 1) * (kTileN / 2); c += kChunk) {
+        if (c0 + c >= a.N) break;                                             // uniform across the warp
+        const int cols = (int)(a.N - c0 - c < kChunk ? a.N - c0 - c : kChunk);
+#pragma unroll
+        for (int half = 0; half < kChunk / 32; ++half) {
+          uint32_t r[32], u[32];
+          tmem_ld32(acc + c + 32 * half, r);
+          if (GATED) tmem_ld32(acc + 128 + c + 32 * half, u);
+          tmem_ld_wait();
+          const float* const dw = &sh->dw[buf][c + 32 * half];
+          const float* const bias = &sh->bias[buf][c + 32 * half];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            float y = (float)(int)r[j] * (dxv * dw[j]);
+            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[j] * (dxv * dw[128 + j])) : y + bias[j];
+            r[j] = __float_as_uint(ok ? y : nan_f());
+          }
+          if (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) stage[lane * 8 + (j ^ (lane & 7))] = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+          } else {
+            uint32_t b[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+              b[j] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              stage[lane * 8 + ((4 * half + j) ^ (lane & 7))] = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+          }
+        }
+        __syncwarp();
+        store_rows<T>(stage, lane, out + row0 * a.ld + c0 + c, a.ld, rows, cols, a.vec);
+        __syncwarp();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->tmem_empty[buf]), 0));
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (sh->abort_flag) {
+    // give-up path: loads (both CTAs' complete on the leader's barriers) and MMAs that nobody has waited for
+    if (threadIdx.x == 0 && rank == 0) {
+      const uint32_t n = sh->issued;
+      for (uint32_t g = n > (uint32_t)kManyStages ? n - kManyStages : 0u; g < n; ++g) {
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&sh->full[g % kManyStages]), (g / kManyStages) & 1) && global_timer_ns() - t0 < a.waits.limit_ns) {}
+      }
+    }
+    if (warp == 1 && rank == 0) {
+      if (elect_one())
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sh->drain)) : "memory");
+      const uint64_t t0 = global_timer_ns();
+      while (!mbar_try_wait(smem_u32(&sh->drain), 0) && global_timer_ns() - t0 < a.waits.limit_ns) {}
+    }
+    __syncthreads();
+  }
+  cluster_sync();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host side
+// Rows of K codes, `ld` bytes apart: boxes of 128 codes x box_rows; what lies beyond K or the last row is filled with zeros.
+bool code_map(CUtensorMap* m, const uint8_t* base, int64_t K, int64_t rows, int64_t ld, int box_rows) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename K, typename A>
+qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t smem_most, unsigned grid, unsigned cluster,
+                         const CUtensorMap (&maps)[3], const A& a, cudaStream_t s) {
+  const int dev = current_device();
+  if (dev < 0) return QM_ERR_UNSUPPORTED;
+  if (!ready[dev]) {
+    QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_most));
+    ready[dev] = true;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  QM_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], a));
+  count_launch();
+  return QM_OK;
+}
+
+Scales scales_of(const LinearArgs& l) {
+  return {l.dx, {l.dw[0], l.dw[1]}, l.bias, l.bias_dtype == QM_DT_BF16, l.act};
+}
+
+constexpr size_t kFewRing = 200 * 1024;
+constexpr size_t kFewSmem = 1024 + kFewRing + sizeof(SharedFew);
+
+template <typename T, bool GATED>
+qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
+  static bool ready[kMaxDevices] = {};
+  FewArgs a{};
+  a.M = l.M; a.N = l.N;
+  a.num_kb = (int)((l.K + kBlock - 1) / kBlock);
+  a.nt = 16;
+  while (a.nt < 128 && a.nt < l.M) a.nt *= 2;
+  const int64_t tiles_m = (l.M + a.nt - 1) / a.nt, tiles = (l.N + kBlock - 1) / kBlock * tiles_m;
+  a.split = 1;
+  while (a.split < kMaxSplit && 2 * a.split <= a.num_kb && tiles * 2 * a.split <= sm_count()) a.split *= 2;
+  const size_t stage = (GATED ? 2 : 1) * kBlockBytes + (size_t)a.nt * kBlock;
+  a.stages = (int)std::min<size_t>(kFewStages, kFewRing / stage);
+  a.tiles_m = (int)tiles_m;
+  a.idesc = make_idesc(2, 1, 1, kBlock, (uint32_t)a.nt);                      // s8 x s8 -> s32
+  a.tmem_cols = std::max(32, a.nt * (GATED ? 2 : 1));
+  a.sc = scales_of(l); a.out = l.out; a.ld = l.ld_out;
+  wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
+  CUtensorMap maps[3];
+  if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, a.nt) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
+  if (!GATED) maps[2] = maps[1];
+  else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
+  return launch_cluster(linear_few_kernel<T, GATED>, ready, 1024 + a.stages * stage + sizeof(SharedFew), kFewSmem,
+                        (unsigned)(tiles * a.split), (unsigned)a.split, maps, a, s);
+}
+
+template <typename T, bool GATED>
+qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
+  static bool ready[kMaxDevices] = {};
+  constexpr size_t smem = 1024 + (size_t)kManyStages * kManyStageBytes + sizeof(SharedMany);
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  ManyArgs a{};
+  a.M = l.M; a.N = l.N;
+  a.num_kb = (int)((l.K + kBlock - 1) / kBlock);
+  a.tiles_n = (int)((l.N + (GATED ? 127 : 255)) / (GATED ? 128 : 256));
+  const int64_t tiles = (l.M + 255) / 256 * a.tiles_n;
+  if (tiles >= (1ll << 31) - 1024) return QM_ERR_UNSUPPORTED;                 // the walk adds the grid to an index
+  a.num_tiles = (int)tiles;
+  a.sc = scales_of(l); a.out = l.out; a.ld = l.ld_out;
+  a.vec = (reinterpret_cast<uintptr_t>(l.out) & 15) == 0 && (l.ld_out * sizeof(T)) % 16 == 0;
+  wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
+  CUtensorMap maps[3];
+  if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, kBlock) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
+  if (!GATED) maps[2] = maps[1];
+  else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
+  const int pairs = sm_count() / 2;
+  return launch_cluster(linear_many_kernel<T, GATED>, ready, smem, smem, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 2u, maps, a, s);
+}
+
+template <typename T, bool GATED>
+qm_status launch_typed(const LinearArgs& l, cudaStream_t s) {
+  return l.M <= 512 ? launch_few<T, GATED>(l, s) : launch_many<T, GATED>(l, s);
 }
 
 }  // namespace
 
-qm_status launch_linear_int8(const LinearArgs& a, cudaStream_t s) {
-  const bool gated = a.w[1] != nullptr, bf16 = a.out_dtype == QM_DT_BF16;
-  auto kern = gated ? (bf16 ? linear_tile<__nv_bfloat16, true> : linear_tile<float, true>)
-                    : (bf16 ? linear_tile<__nv_bfloat16, false> : linear_tile<float, false>);
-  const int64_t tiles_m = (a.M + kTile - 1) / kTile, tiles_n = (a.N + kTile - 1) / kTile;
-  if (tiles_m > 65535) return QM_ERR_UNSUPPORTED;
-  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)tiles_n, (unsigned)tiles_m), dim3(256), 0, s, a));
-  count_launch();
-  return QM_OK;
+qm_status launch_linear_int8(const LinearArgs& l, cudaStream_t s) {
+  const bool gated = l.w[1] != nullptr;
+  if (l.out_dtype == QM_DT_BF16) return gated ? launch_typed<__nv_bfloat16, true>(l, s) : launch_typed<__nv_bfloat16, false>(l, s);
+  return gated ? launch_typed<float, true>(l, s) : launch_typed<float, false>(l, s);
 }
 
 }  // namespace qm

@@ -227,3 +227,37 @@ def test_refusals():
             bad()
     with pytest.raises(KeyError):
         g(x, dx, w, dw, w, dw, 64, act="relu")
+
+
+@pytest.fixture
+def starved_producer():
+    L = qm.lib()
+    L.qm_debug_set_wait_limit_ns(2_000_000)                            # 2 ms instead of 1 s
+    yield L
+    L.qm_debug_stop_producer_after(0xffffffff)
+    L.qm_debug_set_wait_limit_ns(0)
+
+
+# one row split over a cluster (long contractions: every part has several blocks); a few, unsplit (many weight rows); many, one tile
+# and several to a CTA pair
+@pytest.mark.parametrize("M,N,K", [(1, 256, 8192), (40, 256, 4096), (8, 30000, 256), (600, 300, 384), (2500, 2600, 256)])
+@pytest.mark.parametrize("stop_after", [0, 1])
+@pytest.mark.parametrize("gated", [False, True])
+def test_wait_runs_out_and_the_kernel_returns(starved_producer, M, N, K, stop_after, gated):
+    """The loading warp stops on request (nothing is in flight that is never awaited): the waits run into their limit, the outputs
+    that could not be computed are NaN, and the next call is right."""
+    cx, x = codes(M, K, 37)
+    cw, w = codes(N, K, 38)
+    dx, dw = deltas(M, 39, 0.01).cuda(), deltas(N, 40, 0.0001).cuda()
+    call = (lambda: qm.qm_gated_linear_int8(x, dx, w, dw, w, dw, K)) if gated else (lambda: qm.qm_linear_int8(x, dx, w, dw, K))
+    want = call()
+    assert not want.isnan().any()
+    starved_producer.qm_debug_stop_producer_after(stop_after)
+    y = call()
+    torch.cuda.synchronize()
+    bad = y.isnan()
+    assert bad.any() and torch.equal(y[~bad], want[~bad])
+    if stop_after == 0:
+        assert bad.all()
+    starved_producer.qm_debug_stop_producer_after(0xffffffff)
+    assert torch.equal(call(), want)
