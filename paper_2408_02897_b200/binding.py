@@ -3,7 +3,6 @@
 Tensors are torch CUDA tensors (torch is used for device memory and streams); an operand of a
 product L.R is described by `operand_of(tensor, contract_dim)`.
 """
-import contextlib
 import ctypes as C
 import os
 import threading
@@ -290,14 +289,25 @@ def _vector(t, what, n, dtypes, device):
     return t.data_ptr()
 
 
+_current_stream = torch._C._cuda_getCurrentRawStream      # (torch.cuda.current_stream() builds an object: 3 us)
+
+
 def _on(stream):
-    """(device, stream handle, context to allocate in): new tensors belong to the stream that writes them."""
+    """(current device, handle of `stream` or of the current one)"""
     device = torch.cuda.current_device()
     if stream is None:
-        return device, torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
+        return device, _current_stream(device)
     if stream.device_index != device:
         _refuse("the stream is not one of the current CUDA device")
-    return device, stream.cuda_stream, torch.cuda.stream(stream)
+    return device, stream.cuda_stream
+
+
+def _new(like, shape, dtype, stream):
+    """A new tensor beside `like`, which belongs to the stream that writes it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 _FLOATS, _FP32, _BYTES = (torch.bfloat16, torch.float32), (torch.float32,), (torch.uint8,)
@@ -308,25 +318,24 @@ def qm_rms_norm_quantize(x, weight, eps, fmt, residual=None, residual_out=None, 
     residual_out or None).  codes * delta stands for z * weight / rms(z), z = x + residual in x's type, which residual_out
     receives (made here when none is passed; it may be x or residual itself).  x, residual and residual_out are [rows, cols]
     with contiguous rows of any pitch; the codes and scales are what qm_gemm and qm_linear_int8 take."""
-    device, handle, alloc = _on(stream)
+    device, handle = _on(stream)
     rows, cols, ld = _matrix(x, "x", _FLOATS, device)
     dt = x.dtype
     w = _vector(weight, "weight", cols, _FLOATS, device)
     r = z = None
     ld_r = ld_z = 0
-    with alloc:
-        codes = torch.empty((1, rows, qm_code_ld(cols)), dtype=torch.uint8, device=x.device)
-        delta = torch.empty(rows, dtype=torch.float32, device=x.device)
-        if residual is not None:
-            if residual_out is None:
-                residual_out = torch.empty((rows, cols), dtype=dt, device=x.device)
-            r_rows, r_cols, ld_r = _matrix(residual, "residual", (dt,), device)
-            z_rows, z_cols, ld_z = _matrix(residual_out, "residual_out", (dt,), device)
-            if not r_rows == z_rows == rows or not r_cols == z_cols == cols:
-                _refuse("x, residual and residual_out differ in shape")
-            r, z = residual.data_ptr(), residual_out.data_ptr()
-        elif residual_out is not None:
-            _refuse("residual_out without residual")
+    if residual is not None:
+        if residual_out is None:
+            residual_out = _new(x, (rows, cols), dt, stream)
+        r_rows, r_cols, ld_r = _matrix(residual, "residual", (dt,), device)
+        z_rows, z_cols, ld_z = _matrix(residual_out, "residual_out", (dt,), device)
+        if not r_rows == z_rows == rows or not r_cols == z_cols == cols:
+            _refuse("x, residual and residual_out differ in shape")
+        r, z = residual.data_ptr(), residual_out.data_ptr()
+    elif residual_out is not None:
+        _refuse("residual_out without residual")
+    codes = _new(x, (1, rows, qm_code_ld(cols)), torch.uint8, stream)
+    delta = _new(x, (rows,), torch.float32, stream)
     st = lib().qm_rms_norm_quantize(x.data_ptr(), ld, r, ld_r, _DT[dt], w, _DT[weight.dtype], eps, rows, cols, FMT[fmt], z, ld_z,
                                     codes.data_ptr(), delta.data_ptr(), handle)
     if st:
@@ -341,13 +350,11 @@ def _codes(t, what, K, device):
     return rows, max(ld, qm_code_ld(K)) if rows <= 1 else ld
 
 
-def _linear_out(out, out_dtype, M, N, alloc, device):
+def _linear_out(out, out_dtype, M, N, beside, stream, device):
     if out is None:
         if out_dtype not in _DT:
             _refuse("out_dtype: torch.bfloat16 or torch.float32")
-        with alloc:
-            out = torch.empty((M, N), dtype=out_dtype, device=torch.device("cuda", device))
-        return out, N
+        return _new(beside, (M, N), out_dtype, stream), N
     rows, cols, ld = _matrix(out, "out", _FLOATS, device)
     if rows != M or cols != N:
         _refuse(f"out: wants [{M}, {N}]")
@@ -359,12 +366,12 @@ def qm_linear_int8(codes_x, delta_x, codes_w, delta_w, K, bias=None, out_dtype=t
     (codes_x . codes_w^T) * (delta_x outer delta_w) + bias.  codes_x [M, >= K] and codes_w [N, >= K] are rows of INT8 codes
     (uint8 tensors, 2-D or with a leading 1, pitch a multiple of 16), as qm_rms_norm_quantize and qm_quantize(.., "channel")
     leave them; `out` may be a view with any row pitch (its type then counts, not out_dtype)."""
-    device, handle, alloc = _on(stream)
+    device, handle = _on(stream)
     M, ld_x = _codes(codes_x, "codes_x", K, device)
     N, ld_w = _codes(codes_w, "codes_w", K, device)
     dx, dw = _vector(delta_x, "delta_x", M, _FP32, device), _vector(delta_w, "delta_w", N, _FP32, device)
     b = _vector(bias, "bias", N, _FLOATS, device) if bias is not None else None
-    out, ld = _linear_out(out, out_dtype, M, N, alloc, device)
+    out, ld = _linear_out(out, out_dtype, M, N, codes_x, stream, device)
     st = lib().qm_linear_int8(codes_x.data_ptr(), ld_x, dx, codes_w.data_ptr(), ld_w, dw, b,
                               _DT[bias.dtype] if b is not None else 0, M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
     if st:
@@ -376,7 +383,7 @@ def qm_gated_linear_int8(codes_x, delta_x, codes_gate, delta_gate, codes_up, del
                          out=None, stream=None):
     """The gated form act(x . gate^T) * (x . up^T) of qm_linear_int8, one kernel, -> [M, N].  act: "silu", "gelu" or
     "gelu_tanh".  codes_gate and codes_up [N, >= K] may be the halves of one tensor."""
-    device, handle, alloc = _on(stream)
+    device, handle = _on(stream)
     M, ld_x = _codes(codes_x, "codes_x", K, device)
     N, ld_g = _codes(codes_gate, "codes_gate", K, device)
     N_up, ld_u = _codes(codes_up, "codes_up", K, device)
@@ -384,7 +391,7 @@ def qm_gated_linear_int8(codes_x, delta_x, codes_gate, delta_gate, codes_up, del
         _refuse("codes_gate and codes_up differ in their number of rows")
     dx = _vector(delta_x, "delta_x", M, _FP32, device)
     dg, du = _vector(delta_gate, "delta_gate", N, _FP32, device), _vector(delta_up, "delta_up", N, _FP32, device)
-    out, ld = _linear_out(out, out_dtype, M, N, alloc, device)
+    out, ld = _linear_out(out, out_dtype, M, N, codes_x, stream, device)
     st = lib().qm_gated_linear_int8(codes_x.data_ptr(), ld_x, dx, codes_gate.data_ptr(), ld_g, dg, codes_up.data_ptr(), ld_u, du,
                                     ACT[act], M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
     if st:
