@@ -15,6 +15,8 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <cstdio>
+#include <cstdlib>
 
 #include "qm_internal.h"
 #include "tc_ptx.cuh"
@@ -55,23 +57,40 @@ __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 struct FewArgs {
   int64_t M, N;
   int num_kb, tiles_m, split, nt, stages;    // nt: rows of x per tile, 16 .. 128
+  uint32_t sums_bytes;
   uint32_t idesc, tmem_cols;
   Scales sc;
   Waits waits;
   void* out; int64_t ld;
+  int vec;                                   // four outputs at a multiple of four start on as many bytes
 };
 constexpr int kFewStages = 12;
 constexpr int kMaxSplit = 8;
 struct SharedFew {
   uint64_t full[kFewStages], empty[kFewStages], done, drain;
-  uint32_t tmem_base, abort_flag, issued, pad;
+  uint32_t tmem_base, abort_flag, issued, gave_up;     // gave_up: some CTA of the cluster did
   float dx[256];
 };
 
-__device__ __forceinline__ uint32_t lds_cluster(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void sts_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void add4(int4& a, const int4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
+
+__device__ __forceinline__ void store4(float* p, const float (&y)[4], int n, bool vec) {
+  if (vec && n >= 4) *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+  else
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (k < n) p[k] = y[k];
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&y)[4], int n, bool vec) {
+  if (vec && n >= 4) {
+    __nv_bfloat162 h[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
+    *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(h);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (k < n) p[k] = __float2bfloat16_rn(y[k]);
+  }
 }
 
 template <typename T, bool GATED>
@@ -82,7 +101,9 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   constexpr int kW = GATED ? 2 : 1;
   const uint32_t stage_bytes = kW * kBlockBytes + (uint32_t)a.nt * kBlock;
-  SharedFew* sh = reinterpret_cast<SharedFew*>(tiles + (size_t)a.stages * stage_bytes);
+  // behind the ring: of a split contraction the parts' sums of this CTA's rows, [part][product][row][weight row]
+  int* const sums = reinterpret_cast<int*>(tiles + (size_t)a.stages * stage_bytes);
+  SharedFew* sh = reinterpret_cast<SharedFew*>(reinterpret_cast<uint8_t*>(sums) + a.sums_bytes);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split;
   const int n0 = tile / a.tiles_m * kBlock, m0 = tile % a.tiles_m * a.nt;
@@ -100,7 +121,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     }
     mbar_init(smem_u32(&sh->done), 1);
     mbar_init(smem_u32(&sh->drain), 1);
-    sh->abort_flag = 0; sh->issued = 0;
+    sh->abort_flag = 0; sh->issued = 0; sh->gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -111,6 +132,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   }
   tc_fence_before();
   __syncthreads();
+  if (a.split > 1) cluster_arrive();               // this CTA's shared memory may be written by its peers
   pdl_prologue();
   tc_fence_after();
   const uint32_t tmem_base = sh->tmem_base;
@@ -157,21 +179,30 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   }
 
   // epilogue, warps 2..9: a warp may read the quarter warp % 4 of tensor memory's lanes; the two warps of a quarter take every
-  // other chunk of 16 columns (rows of x)
+  // other chunk of 16 columns (rows of x).  Scales and biases are fetched ahead of the waits.
   const int et = (int)threadIdx.x - 64, q = warp & 3, h = (warp - 2) >> 2;
   const int live = (int)(a.M - m0 < a.nt ? a.M - m0 : a.nt);                 // rows of x in this tile
+  // of a split contraction a CTA finishes `own` rows of x, a thread four neighbouring weight rows at a time
+  const int own = (live + a.split - 1) / a.split;
+  const int j = a.split == 1 ? q * 32 + lane : 4 * (et & (kBlock / 4 - 1));
   T* const out = static_cast<T*>(a.out);
+  float dw[4], du[4], bias[4];
   if (warp >= 2) {
     if (et < live) sh->dx[et] = a.sc.dx[m0 + et];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t n = (int64_t)n0 + j + k;
+      const bool in = n < a.N && (k == 0 || a.split > 1);
+      dw[k] = in ? a.sc.dw[0][n] : 0.f;
+      du[k] = GATED && in ? a.sc.dw[1][n] : 0.f;
+      bias[k] = !GATED && in ? load_bias(a.sc, n) : 0.f;
+    }
     const bool ok = w.wait_warp(smem_u32(&sh->done), 0);
     tc_fence_after();
     asm volatile("bar.sync 1, 256;" ::: "memory");                            // dx is there, and every warp has waited
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
-    const int j = q * 32 + lane;
-    const int64_t n = (int64_t)n0 + j;
     if (a.split == 1) {
-      const bool col = n < a.N;
-      const float dw = col ? a.sc.dw[0][n] : 0.f, du = GATED && col ? a.sc.dw[1][n] : 0.f, bias = !GATED && col ? load_bias(a.sc, n) : 0.f;
+      const int64_t n = (int64_t)n0 + j;
       for (int c = h * 16; c < live; c += 32) {
         uint32_t r[16], u[16];
         if (ok) {
@@ -181,57 +212,61 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (col && c + i < live) {
+          if (n < a.N && c + i < live) {
             const float dxv = sh->dx[c + i];
-            float y = (float)(int)r[i] * (dxv * dw);
-            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[i] * (dxv * du)) : y + bias;
+            float y = (float)(int)r[i] * (dxv * dw[0]);
+            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[i] * (dxv * du[0])) : y + bias[0];
             out[(int64_t)(m0 + c + i) * a.ld + n] = (T)(ok ? y : nan_f());
           }
       }
     } else {
-      // this CTA's share of the sums, [row of x][weight row], for the cluster: the ring is not in use any more
-      int* const sums = reinterpret_cast<int*>(tiles);
+      // this part's sums to the CTAs that finish their rows: stores to another SM's shared memory are not waited for one by one,
+      // as reads are (1 row of 4096 weight rows 0.7 us, 64 rows 1.4)
+      cluster_wait();
+      if (!ok && lane < a.split) sts_cluster(map_to_cta(smem_u32(&sh->gave_up), lane), 1u);
       for (int c = h * 16; ok && c < live; c += 32) {
 #pragma unroll
         for (int p = 0; p < kW; ++p) {
           uint32_t r[16];
           tmem_ld16(lane_addr + p * a.nt + c, r);
           tmem_ld_wait();
+          int owner = c / own, row = c - owner * own;
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (c + i < live) sums[(p * a.nt + c + i) * kBlock + j] = (int)r[i];
+            if (c + i < live) {
+              sts_cluster(map_to_cta(smem_u32(sums + ((part * kW + p) * own + row) * kBlock + q * 32 + lane), owner), r[i]);
+              if (++row == own) { row = 0; ++owner; }
+            }
         }
       }
     }
   }
   if (a.split > 1) {
-    __syncthreads();
+    if (warp < 2) cluster_wait();
     cluster_sync();
-    if (warp >= 2) {
-      bool ok = true;
-      for (int p = 0; p < a.split; ++p) ok = ok && lds_cluster(map_to_cta(smem_u32(&sh->abort_flag), p)) == 0;
-      const int total = live * kBlock, share = ((total + a.split - 1) / a.split + 31) & ~31;
-      const int end = min(total, (part + 1) * share);
-      const int j = (part * share + et) & (kBlock - 1);                       // the same for all elements of a thread
-      const int64_t n = (int64_t)n0 + j;
-      if (n < a.N) {
-        const float dw = a.sc.dw[0][n], du = GATED ? a.sc.dw[1][n] : 0.f, bias = !GATED ? load_bias(a.sc, n) : 0.f;
-        const uint32_t mine = smem_u32(tiles);
-        for (int e = part * share + et; e < end; e += 256) {
-          int g = 0, u = 0;
+    const int cols = (int)(a.N - n0 - j < 4 ? a.N - n0 - j : 4);
+    if (warp >= 2 && cols > 0) {
+      const bool ok = sh->gave_up == 0;
+      const int rows = min(own, live - part * own);
+      for (int i = et / (kBlock / 4); i < rows; i += 256 / (kBlock / 4)) {
+        int4 g = make_int4(0, 0, 0, 0), u = g;
 #pragma unroll
-          for (int p = 0; p < kMaxSplit; ++p)
-            if (p < a.split) {
-              const uint32_t peer = map_to_cta(mine, p);
-              g += (int)lds_cluster(peer + 4 * e);
-              if (GATED) u += (int)lds_cluster(peer + 4 * (a.nt * kBlock + e));
-            }
-          const int i = e / kBlock;
-          const float dxv = sh->dx[i];
-          float y = (float)g * (dxv * dw);
-          y = GATED ? activate(y, a.sc.act) * ((float)u * (dxv * du)) : y + bias;
-          out[(int64_t)(m0 + i) * a.ld + n] = (T)(ok ? y : nan_f());
+        for (int p = 0; p < kMaxSplit; ++p)
+          if (p < a.split) {
+            add4(g, *reinterpret_cast<const int4*>(sums + (p * kW * own + i) * kBlock + j));
+            if (GATED) add4(u, *reinterpret_cast<const int4*>(sums + ((p * kW + 1) * own + i) * kBlock + j));
+          }
+        const int row = part * own + i;
+        const float dxv = sh->dx[row];
+        const int gs[4] = {g.x, g.y, g.z, g.w}, us[4] = {u.x, u.y, u.z, u.w};
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          y[k] = (float)gs[k] * (dxv * dw[k]);
+          y[k] = GATED ? activate(y[k], a.sc.act) * ((float)us[k] * (dxv * du[k])) : y[k] + bias[k];
+          if (!ok) y[k] = nan_f();
         }
+        store4(out + (int64_t)(m0 + row) * a.ld + n0 + j, y, cols, a.vec);
       }
     }
   }
@@ -254,7 +289,6 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     }
     __syncthreads();
   }
-  if (a.split > 1) cluster_sync();              // the peers have read this CTA's sums
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -276,9 +310,50 @@ constexpr uint32_t kManyStageBytes = 2 * kBlockBytes;
 struct SharedMany {
   uint64_t full[kManyStages], empty[kManyStages], tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base, abort_flag, issued, pad;
-  float dw[2][256], bias[2][256];
-  uint4 stage[kEpiWarps][32 * 8];              // 32 rows of 128 bytes of output per epilogue warp
+  alignas(16) float dw[2][256], bias[2][256];
+  alignas(16) uint4 stage[kEpiWarps][32 * 8];  // 32 rows of 128 bytes of output per epilogue warp
 };
+
+// 16 lanes x 32 columns of tensor memory: thread t gets, of every 8 columns i, columns 2 (t % 4) and one more in lanes t / 4 (words 4 i,
+// 4 i + 1) and t / 4 + 8 (4 i + 2, 4 i + 3).
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+        "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+
+// 16 rows (from `row`) x 32 columns (from `col`) of output in that layout to the warp's staging buffer: rows of 128 bytes, 16-byte
+// units permuted with the row.
+__device__ __forceinline__ void stage_16x32(uint32_t stage, int lane, int row, int col, const float (&y)[16], float) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh) {
+      const int r = row + 8 * hh + (lane >> 2), unit = col / 4 + 2 * i + ((lane >> 1) & 1);
+      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stage + r * 128 + ((unit ^ (r & 7)) << 4) + (lane & 1) * 8),
+                   "f"(y[4 * i + 2 * hh]), "f"(y[4 * i + 2 * hh + 1]) : "memory");
+    }
+}
+__device__ __forceinline__ void stage_16x32(uint32_t stage, int lane, int row, int col, const float (&y)[16], __nv_bfloat16) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    uint32_t w[4];                                          // two 8-column groups, the upper and lower 8 rows of each
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int k = 4 * (2 * j + (m >> 1)) + 2 * (m & 1);
+      const __nv_bfloat162 v = __floats2bfloat162_rn(y[k], y[k + 1]);
+      w[m] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    const int m = lane >> 3, r = row + 8 * (m & 1) + (lane & 7), unit = col / 8 + 2 * j + (m >> 1);
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(stage + r * 128 + ((unit ^ (r & 7)) << 4)),
+                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+  }
+}
 
 // The warp's 32 rows x 128 bytes of output out of shared memory, whole lines per instruction (16-byte units permuted with the row:
 // conflict-free both ways); ragged chunks and rows that do not start on 16 bytes an element per lane.
@@ -394,11 +469,12 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       }
     }
   } else {
-    // epilogue, warps 2..9 of both CTAs: a row of x per lane; the two warps of a lane quarter take half of the columns each
+    // epilogue, warps 2..9 of both CTAs; the two warps of a lane quarter (32 rows of x) take half of the columns each
     const int q = warp & 3, h = (warp - 2) >> 2, et = (int)threadIdx.x - 64;
     uint4* const stage = sh->stage[warp - 2];
     T* const out = static_cast<T*>(a.out);
     constexpr int kChunk = 128 / sizeof(T);
+    const bool has_bias = a.sc.bias != nullptr;
     bool ok = true;
     uint32_t it = 0;
     for (int t = pair; t < a.num_tiles; t += num_pairs, ++it) {
@@ -412,9 +488,11 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         sh->dw[buf][et] = !in ? 0.f : GATED && et >= 128 ? a.sc.dw[1][col] : a.sc.dw[0][col];
         if (!GATED) sh->bias[buf][et] = in ? load_bias(a.sc, col) : 0.f;
       }
-      const int64_t row0 = (int64_t)tm * 256 + rank * kBlock + q * 32, row = row0 + lane;
+      const int64_t row0 = (int64_t)tm * 256 + rank * kBlock + q * 32;
       const int rows = (int)(a.M - row0 < 32 ? a.M - row0 : 32);             // <= 0: none
-      const float dxv = row < a.M ? a.sc.dx[row] : 0.f;
+      float dx[4];                                                            // of rows lane / 4, + 8, + 16, + 24
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dx[k] = 8 * k + (lane >> 2) < rows ? a.sc.dx[row0 + 8 * k + (lane >> 2)] : 0.f;
       ok = ok && w.wait_warp(smem_u32(&sh->tmem_full[buf]), (it >> 1) & 1);
       asm volatile("bar.sync 1, 256;" ::: "memory");                          // publishes the scales
       tc_fence_after();
@@ -424,32 +502,36 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         if (c0 + c >= a.N) break;                                             // uniform across the warp
         const int cols = (int)(a.N - c0 - c < kChunk ? a.N - c0 - c : kChunk);
 #pragma unroll
-        for (int half = 0; half < kChunk / 32; ++half) {
-          uint32_t r[32], u[32];
-          tmem_ld32(acc + c + 32 * half, r);
-          if (GATED) tmem_ld32(acc + 128 + c + 32 * half, u);
-          tmem_ld_wait();
-          const float* const dw = &sh->dw[buf][c + 32 * half];
-          const float* const bias = &sh->bias[buf][c + 32 * half];
+        for (int part = 0; part < kChunk; part += 32) {
+          uint32_t r[2][16], u[2][16];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float y = (float)(int)r[j] * (dxv * dw[j]);
-            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[j] * (dxv * dw[128 + j])) : y + bias[j];
-            r[j] = __float_as_uint(ok ? y : nan_f());
+          for (int hf = 0; hf < 2; ++hf) {
+            tmem_ld_16x32(acc + (uint32_t)(hf * 16 << 16) + c + part, r[hf]);
+            if (GATED) tmem_ld_16x32(acc + (uint32_t)(hf * 16 << 16) + 128 + c + part, u[hf]);
           }
-          if (sizeof(T) == 4) {
+          // a thread has eight columns of four rows: eight scales to load, where a row to a thread takes 32 and the epilogue the
+          // shared memory's bandwidth from the MMAs (16384 x 4096 x 1024 61 us so)
+          float2 d[4], e[4], b[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) stage[lane * 8 + (j ^ (lane & 7))] = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
-          } else {
-            uint32_t b[16];
+          for (int i = 0; i < 4; ++i) {
+            const int k = c + part + 8 * i + 2 * (lane & 3);
+            d[i] = *reinterpret_cast<const float2*>(&sh->dw[buf][k]);
+            if (GATED) e[i] = *reinterpret_cast<const float2*>(&sh->dw[buf][128 + k]);
+            b[i] = !GATED && has_bias ? *reinterpret_cast<const float2*>(&sh->bias[buf][k]) : make_float2(0.f, 0.f);
+          }
+          tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-              b[j] = *reinterpret_cast<const uint32_t*>(&v);
+          for (int hf = 0; hf < 2; ++hf) {
+            float y[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const int i = k >> 2;
+              const float dxv = dx[2 * hf + ((k >> 1) & 1)];
+              y[k] = (float)(int)r[hf][k] * (dxv * (k & 1 ? d[i].y : d[i].x));
+              y[k] = GATED ? activate(y[k], a.sc.act) * ((float)(int)u[hf][k] * (dxv * (k & 1 ? e[i].y : e[i].x))) : y[k] + (k & 1 ? b[i].y : b[i].x);
+              if (!ok) y[k] = nan_f();
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              stage[lane * 8 + ((4 * half + j) ^ (lane & 7))] = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+            stage_16x32(smem_u32(stage), lane, 16 * hf, part, y, T());
           }
         }
         __syncwarp();
@@ -535,23 +617,31 @@ qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
   FewArgs a{};
   a.M = l.M; a.N = l.N;
   a.num_kb = (int)((l.K + kBlock - 1) / kBlock);
+  int e_nt=0,e_split=0,e_st=0; if(const char*e=getenv("QM_FEW")) sscanf(e,"%d,%d,%d",&e_nt,&e_split,&e_st);
   a.nt = 16;
   while (a.nt < 128 && a.nt < l.M) a.nt *= 2;
+  if(e_nt) a.nt=e_nt;
   const int64_t tiles_m = (l.M + a.nt - 1) / a.nt, tiles = (l.N + kBlock - 1) / kBlock * tiles_m;
   a.split = 1;
   while (a.split < kMaxSplit && 2 * a.split <= a.num_kb && tiles * 2 * a.split <= sm_count()) a.split *= 2;
+  if(e_split) a.split=std::min(e_split,a.num_kb);
   const size_t stage = (GATED ? 2 : 1) * kBlockBytes + (size_t)a.nt * kBlock;
   a.stages = (int)std::min<size_t>(kFewStages, kFewRing / stage);
+  if(e_st) a.stages=std::min(e_st,a.stages);
+  a.sums_bytes = a.split > 1 ? (uint32_t)((GATED ? 2 : 1) * (a.nt + a.split - 1) * kBlock * 4) : 0u;
+  a.stages = std::min(a.stages, (a.num_kb + a.split - 1) / a.split);
+  while (a.stages*stage+a.sums_bytes > kFewRing) --a.stages;
   a.tiles_m = (int)tiles_m;
   a.idesc = make_idesc(2, 1, 1, kBlock, (uint32_t)a.nt);                      // s8 x s8 -> s32
   a.tmem_cols = std::max(32, a.nt * (GATED ? 2 : 1));
   a.sc = scales_of(l); a.out = l.out; a.ld = l.ld_out;
+  a.vec = (reinterpret_cast<uintptr_t>(l.out) & (4 * sizeof(T) - 1)) == 0 && l.ld_out % 4 == 0;
   wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
   CUtensorMap maps[3];
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, a.nt) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
-  return launch_cluster(linear_few_kernel<T, GATED>, ready, 1024 + a.stages * stage + sizeof(SharedFew), kFewSmem,
+  return launch_cluster(linear_few_kernel<T, GATED>, ready, 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), kFewSmem,
                         (unsigned)(tiles * a.split), (unsigned)a.split, maps, a, s);
 }
 
@@ -580,7 +670,8 @@ qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
 
 template <typename T, bool GATED>
 qm_status launch_typed(const LinearArgs& l, cudaStream_t s) {
-  return l.M <= 512 ? launch_few<T, GATED>(l, s) : launch_many<T, GATED>(l, s);
+  int few = l.M <= 512; if(const char*e=getenv("QM_KIND")) few = atoi(e);
+  return few ? launch_few<T, GATED>(l, s) : launch_many<T, GATED>(l, s);
 }
 
 }  // namespace
