@@ -33,19 +33,19 @@ struct Scales {
   const float* dx;
   const float* dw[2];
   const void* bias; int bias_bf16;
-  int act;
 };
 struct Waits { uint64_t limit_ns; uint32_t stop_after; };
 
 // act(g) in fp32.  The tanh form is g / (1 + exp(-2 t)), t the tanh's argument: 1/2 (1 + tanh t) is that quotient, and
 // unlike 1 + tanh(t) it keeps its relative precision where t is negative.  Both sides of the quotient are scaled by
 // 2^-20, because the fast division takes denominators below 2^126; beyond exp's range the quotient is 0.
-__device__ __forceinline__ float activate(float g, int act) {
-  if (act == QM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
-  const float t = act == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
+constexpr int kNoAct = -1;       // one product; the gated kernels are compiled for each activation (see the many rows' epilogue)
+template <int ACT>
+__device__ __forceinline__ float activate(float g) {
+  if (ACT == QM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+  const float t = ACT == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
   return __fdividef(g * 9.5367432e-7f, fmaf(__expf(-t), 9.5367432e-7f, 9.5367432e-7f));
 }
-
 __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
   if (!s.bias) return 0.f;
   return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
@@ -93,10 +93,11 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&y)[4], in
   }
 }
 
-template <typename T, bool GATED>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                   const __grid_constant__ CUtensorMap map_u, const FewArgs a) {
+  constexpr bool GATED = ACT != kNoAct;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   constexpr int kW = GATED ? 2 : 1;
@@ -210,14 +211,21 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
           if (GATED) tmem_ld16(lane_addr + a.nt + c, u);
           tmem_ld_wait();
         }
+        float y[16], up[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (n < a.N && c + i < live) {
-            const float dxv = sh->dx[c + i];
-            float y = (float)(int)r[i] * (dxv * dw[0]);
-            y = GATED ? activate(y, a.sc.act) * ((float)(int)u[i] * (dxv * du[0])) : y + bias[0];
-            out[(int64_t)(m0 + c + i) * a.ld + n] = (T)(ok ? y : nan_f());
-          }
+        for (int i = 0; i < 16; ++i) {
+          const float dxv = sh->dx[c + i];                                    // (rows beyond the last: not stored)
+          y[i] = (float)(int)r[i] * (dxv * dw[0]);
+          if (GATED) up[i] = (float)(int)u[i] * (dxv * du[0]);
+          else y[i] += bias[0];
+        }
+        if (GATED)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i] = activate<ACT>(y[i]) * up[i];
+        T* p = out + (int64_t)(m0 + c) * a.ld + n;
+#pragma unroll
+        for (int i = 0; i < 16; ++i, p += a.ld)
+          if (n < a.N && c + i < live) *p = (T)(ok ? y[i] : nan_f());
       }
     } else {
       // this part's sums to the CTAs that finish their rows: stores to another SM's shared memory are not waited for one by one,
@@ -259,13 +267,18 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         const int row = part * own + i;
         const float dxv = sh->dx[row];
         const int gs[4] = {g.x, g.y, g.z, g.w}, us[4] = {u.x, u.y, u.z, u.w};
-        float y[4];
+        float y[4], up[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           y[k] = (float)gs[k] * (dxv * dw[k]);
-          y[k] = GATED ? activate(y[k], a.sc.act) * ((float)us[k] * (dxv * du[k])) : y[k] + bias[k];
-          if (!ok) y[k] = nan_f();
+          if (GATED) up[k] = (float)us[k] * (dxv * du[k]);
+          else y[k] += bias[k];
         }
+        if (GATED)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = activate<ACT>(y[k]) * up[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (!ok) y[k] = nan_f();
         store4(out + (int64_t)(m0 + row) * a.ld + n0 + j, y, cols, a.vec);
       }
     }
@@ -376,10 +389,11 @@ __device__ __forceinline__ void store_rows(const uint4* stage, int lane, T* out,
   }
 }
 
-template <typename T, bool GATED>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                    const __grid_constant__ CUtensorMap map_u, const ManyArgs a) {
+  constexpr bool GATED = ACT != kNoAct;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   SharedMany* sh = reinterpret_cast<SharedMany*>(tiles + (size_t)kManyStages * kManyStageBytes);
@@ -477,22 +491,31 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const bool has_bias = a.sc.bias != nullptr;
     bool ok = true;
     uint32_t it = 0;
+    // A tile's scales are fetched while the tile before it is written (fetched when they are needed they are 2000 of 6300 cycles a
+    // tile): by column of the accumulators (gated: gate's, then up's) one a thread, and those of rows lane / 4, + 8, + 16, + 24.
+    float next_dw = 0.f, next_bias = 0.f, next_dx[4] = {};
+    auto fetch = [&](int t) {
+      if (t >= a.num_tiles) return;
+      const int tm = t / a.tiles_n;
+      const int64_t col = (int64_t)(t - tm * a.tiles_n) * kTileN + (GATED ? et & 127 : et);
+      const bool in = col < a.N;
+      next_dw = !in ? 0.f : GATED && et >= 128 ? a.sc.dw[1][col] : a.sc.dw[0][col];
+      if (!GATED && has_bias) next_bias = in ? load_bias(a.sc, col) : 0.f;
+      const int64_t row = (int64_t)tm * 256 + rank * kBlock + q * 32 + (lane >> 2);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) next_dx[k] = row + 8 * k < a.M ? a.sc.dx[row + 8 * k] : 0.f;
+    };
+    fetch(pair);
     for (int t = pair; t < a.num_tiles; t += num_pairs, ++it) {
       const int tm = t / a.tiles_n;
       const uint32_t buf = it & 1;
       const int64_t c0 = (int64_t)(t - tm * a.tiles_n) * kTileN;
-      {
-        // column scales by accumulator column (gated: gate's, then up's)
-        const int64_t col = c0 + (GATED ? et & 127 : et);
-        const bool in = col < a.N;
-        sh->dw[buf][et] = !in ? 0.f : GATED && et >= 128 ? a.sc.dw[1][col] : a.sc.dw[0][col];
-        if (!GATED) sh->bias[buf][et] = in ? load_bias(a.sc, col) : 0.f;
-      }
+      sh->dw[buf][et] = next_dw;
+      if (!GATED) sh->bias[buf][et] = next_bias;
+      const float dx[4] = {next_dx[0], next_dx[1], next_dx[2], next_dx[3]};
+      fetch(t + num_pairs);
       const int64_t row0 = (int64_t)tm * 256 + rank * kBlock + q * 32;
       const int rows = (int)(a.M - row0 < 32 ? a.M - row0 : 32);             // <= 0: none
-      float dx[4];                                                            // of rows lane / 4, + 8, + 16, + 24
-#pragma unroll
-      for (int k = 0; k < 4; ++k) dx[k] = 8 * k + (lane >> 2) < rows ? a.sc.dx[row0 + 8 * k + (lane >> 2)] : 0.f;
       ok = ok && w.wait_warp(smem_u32(&sh->tmem_full[buf]), (it >> 1) & 1);
       asm volatile("bar.sync 1, 256;" ::: "memory");                          // publishes the scales
       tc_fence_after();
@@ -522,15 +545,20 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           tmem_ld_wait();
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            float y[16];
+            float y[16], up[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               const int i = k >> 2;
               const float dxv = dx[2 * hf + ((k >> 1) & 1)];
               y[k] = (float)(int)r[hf][k] * (dxv * (k & 1 ? d[i].y : d[i].x));
-              y[k] = GATED ? activate(y[k], a.sc.act) * ((float)(int)u[hf][k] * (dxv * (k & 1 ? e[i].y : e[i].x))) : y[k] + (k & 1 ? b[i].y : b[i].x);
-              if (!ok) y[k] = nan_f();
+              if (GATED) up[k] = (float)(int)u[hf][k] * (dxv * (k & 1 ? e[i].y : e[i].x));
+              else y[k] += k & 1 ? b[i].y : b[i].x;
             }
+            if (GATED)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) y[k] = activate<ACT>(y[k]) * up[k];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) if (!ok) y[k] = nan_f();
             stage_16x32(smem_u32(stage), lane, 16 * hf, part, y, T());
           }
         }
@@ -605,14 +633,15 @@ qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t
 }
 
 Scales scales_of(const LinearArgs& l) {
-  return {l.dx, {l.dw[0], l.dw[1]}, l.bias, l.bias_dtype == QM_DT_BF16, l.act};
+  return {l.dx, {l.dw[0], l.dw[1]}, l.bias, l.bias_dtype == QM_DT_BF16};
 }
 
 constexpr size_t kFewRing = 200 * 1024;
 constexpr size_t kFewSmem = 1024 + kFewRing + sizeof(SharedFew);
 
-template <typename T, bool GATED>
+template <typename T, int ACT>
 qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
+  constexpr bool GATED = ACT != kNoAct;
   static bool ready[kMaxDevices] = {};
   FewArgs a{};
   a.M = l.M; a.N = l.N;
@@ -641,12 +670,13 @@ qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, a.nt) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
-  return launch_cluster(linear_few_kernel<T, GATED>, ready, 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), kFewSmem,
+  return launch_cluster(linear_few_kernel<T, ACT>, ready, 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), kFewSmem,
                         (unsigned)(tiles * a.split), (unsigned)a.split, maps, a, s);
 }
 
-template <typename T, bool GATED>
+template <typename T, int ACT>
 qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
+  constexpr bool GATED = ACT != kNoAct;
   static bool ready[kMaxDevices] = {};
   constexpr size_t smem = 1024 + (size_t)kManyStages * kManyStageBytes + sizeof(SharedMany);
   static_assert(smem <= 232448, "shared memory of a CTA");
@@ -665,21 +695,26 @@ qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
   const int pairs = sm_count() / 2;
-  return launch_cluster(linear_many_kernel<T, GATED>, ready, smem, smem, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 2u, maps, a, s);
+  return launch_cluster(linear_many_kernel<T, ACT>, ready, smem, smem, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 2u, maps, a, s);
 }
 
-template <typename T, bool GATED>
-qm_status launch_typed(const LinearArgs& l, cudaStream_t s) {
+template <typename T, int ACT>
+qm_status launch_sized(const LinearArgs& l, cudaStream_t s) {
   int few = l.M <= 512; if(const char*e=getenv("QM_KIND")) few = atoi(e);
-  return few ? launch_few<T, GATED>(l, s) : launch_many<T, GATED>(l, s);
+  return few ? launch_few<T, ACT>(l, s) : launch_many<T, ACT>(l, s);
+}
+
+template <typename T>
+qm_status launch_typed(const LinearArgs& l, cudaStream_t s) {
+  if (!l.w[1]) return launch_sized<T, kNoAct>(l, s);
+  if (l.act == QM_ACT_SILU) return launch_sized<T, QM_ACT_SILU>(l, s);
+  return l.act == QM_ACT_GELU ? launch_sized<T, QM_ACT_GELU>(l, s) : launch_sized<T, QM_ACT_GELU_TANH>(l, s);
 }
 
 }  // namespace
 
 qm_status launch_linear_int8(const LinearArgs& l, cudaStream_t s) {
-  const bool gated = l.w[1] != nullptr;
-  if (l.out_dtype == QM_DT_BF16) return gated ? launch_typed<__nv_bfloat16, true>(l, s) : launch_typed<__nv_bfloat16, false>(l, s);
-  return gated ? launch_typed<float, true>(l, s) : launch_typed<float, false>(l, s);
+  return l.out_dtype == QM_DT_BF16 ? launch_typed<__nv_bfloat16>(l, s) : launch_typed<float>(l, s);
 }
 
 }  // namespace qm
