@@ -36,16 +36,39 @@ struct Scales {
 };
 struct Waits { uint64_t limit_ns; uint32_t stop_after; };
 
-// act(g) in fp32.  The tanh form is g / (1 + exp(-2 t)), t the tanh's argument: 1/2 (1 + tanh t) is that quotient, and
-// unlike 1 + tanh(t) it keeps its relative precision where t is negative.  Both sides of the quotient are scaled by
-// 2^-20, because the fast division takes denominators below 2^126; beyond exp's range the quotient is 0.
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 constexpr int kNoAct = -1;       // one product; the gated kernels are compiled for each activation (see the many rows' epilogue)
+// act(g) in fp32.
+//  GELU: g Phi(g), Phi(-|g|) = erfc(z) / 2 with z = |g| / sqrt 2 and erfc(z) = t exp(-z^2 + Q(t)), t = 1 / (1 + 0.39 z).  Q is log(erfc(z)
+//    exp(z^2) / t) interpolated at Chebyshev points for z up to 10, degree 8: 6.3e-8 off, which with fp32's roundings is 4.2 half steps of |g|
+//    (erff and 1 + erf are as many, in three times the instructions).  To the base 2, with |g| for z.
+//  The others: g / (1 + exp(-t)), t = g or twice the tanh's argument: 1/2 (1 + tanh) is that quotient, and unlike 1 + tanh it keeps
+//    its relative precision where g is negative.  Both sides of the quotient are scaled by 2^-20, because the approximate
+//    reciprocal gives 0 from 2^126 on; beyond exp's range the quotient is 0.
 template <int ACT>
 __device__ __forceinline__ float activate(float g) {
-  if (ACT == QM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+  if (ACT == QM_ACT_GELU) {
+    const float t = rcp_approx(fmaf(0.27577165f, fabsf(g), 1.f));
+    float q = -0.33402064f;
+    q = fmaf(q, t, 1.5611439f); q = fmaf(q, t, -2.708909f); q = fmaf(q, t, 2.1119456f); q = fmaf(q, t, -1.0494819f);
+    q = fmaf(q, t, 0.6094263f); q = fmaf(q, t, 0.5445073f); q = fmaf(q, t, 1.4499226f); q = fmaf(q, t, -2.1845343f);
+    const float half = 0.5f * g, tail = half * (t * ex2_approx(fmaf(g * g, -0.72134752f, q)));
+    return g < 0.f ? tail : g - tail;
+  }
   const float t = ACT == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
-  return __fdividef(g * 9.5367432e-7f, fmaf(__expf(-t), 9.5367432e-7f, 9.5367432e-7f));
+  return g * 9.5367432e-7f * rcp_approx(fmaf(ex2_approx(-1.442695f * t), 9.5367432e-7f, 9.5367432e-7f));
 }
+
 __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
   if (!s.bias) return 0.f;
   return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
