@@ -81,6 +81,7 @@ struct FewArgs {
   int64_t M, N;
   int num_kb, tiles_m, split, nt, stages;    // nt: rows of x per tile, 16 .. 128
   uint32_t sums_bytes;
+  int own_log2;                              // of a split contraction, rows of x that a CTA of the cluster finishes
   uint32_t idesc, tmem_cols;
   Scales sc;
   Waits waits;
@@ -207,7 +208,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   const int et = (int)threadIdx.x - 64, q = warp & 3, h = (warp - 2) >> 2;
   const int live = (int)(a.M - m0 < a.nt ? a.M - m0 : a.nt);                 // rows of x in this tile
   // of a split contraction a CTA finishes `own` rows of x, a thread four neighbouring weight rows at a time
-  const int own = (live + a.split - 1) / a.split;
+  const int own = 1 << a.own_log2;
   const int j = a.split == 1 ? q * 32 + lane : 4 * (et & (kBlock / 4 - 1));
   T* const out = static_cast<T*>(a.out);
   float dw[4], du[4], bias[4];
@@ -261,13 +262,17 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
           uint32_t r[16];
           tmem_ld16(lane_addr + p * a.nt + c, r);
           tmem_ld_wait();
-          int owner = c / own, row = c - owner * own;
+          const uint32_t at = smem_u32(sums + (part * kW + p) * own * kBlock + q * 32 + lane);
+          if (own >= 16) {                                                    // one CTA's rows, from c & (own - 1) on
+            const uint32_t to = map_to_cta(at, c >> a.own_log2) + (uint32_t)((c & (own - 1)) * kBlock * 4);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c + i < live) {
-              sts_cluster(map_to_cta(smem_u32(sums + ((part * kW + p) * own + row) * kBlock + q * 32 + lane), owner), r[i]);
-              if (++row == own) { row = 0; ++owner; }
-            }
+            for (int i = 0; i < 16; ++i)
+              if (c + i < live) sts_cluster(to + i * kBlock * 4, r[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (c + i < live) sts_cluster(map_to_cta(at, (c + i) >> a.own_log2) + (uint32_t)((i & (own - 1)) * kBlock * 4), r[i]);
+          }
         }
       }
     }
@@ -281,12 +286,13 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       const int rows = min(own, live - part * own);
       for (int i = et / (kBlock / 4); i < rows; i += 256 / (kBlock / 4)) {
         int4 g = make_int4(0, 0, 0, 0), u = g;
-#pragma unroll
-        for (int p = 0; p < kMaxSplit; ++p)
-          if (p < a.split) {
-            add4(g, *reinterpret_cast<const int4*>(sums + (p * kW * own + i) * kBlock + j));
-            if (GATED) add4(u, *reinterpret_cast<const int4*>(sums + ((p * kW + 1) * own + i) * kBlock + j));
-          }
+        const int4* from = reinterpret_cast<const int4*>(sums + i * kBlock + j);
+        const int next = kW * own * (kBlock / 4);                             // from a part to the one behind it
+#pragma unroll 2
+        for (int p = 0; p < a.split; ++p, from += next) {
+          add4(g, *from);
+          if (GATED) add4(u, from[own * (kBlock / 4)]);
+        }
         const int row = part * own + i;
         const float dxv = sh->dx[row];
         const int gs[4] = {g.x, g.y, g.z, g.w}, us[4] = {u.x, u.y, u.z, u.w};
@@ -343,11 +349,11 @@ struct ManyArgs {
 };
 constexpr int kManyStages = 5;
 constexpr uint32_t kManyStageBytes = 2 * kBlockBytes;
+constexpr uint32_t kOutBytes = 32 * 128;       // of output on its way per epilogue warp: 32 rows of 128 bytes
 struct SharedMany {
   uint64_t full[kManyStages], empty[kManyStages], tmem_full[2], tmem_empty[2], drain;
   uint32_t tmem_base, abort_flag, issued, pad;
   alignas(16) float dw[2][256], bias[2][256];
-  alignas(16) uint4 stage[kEpiWarps][32 * 8];  // 32 rows of 128 bytes of output per epilogue warp
 };
 
 // 16 lanes x 32 columns of tensor memory: thread t gets, of every 8 columns i, columns 2 (t % 4) and one more in lanes t / 4 (words 4 i,
@@ -391,43 +397,40 @@ __device__ __forceinline__ void stage_16x32(uint32_t stage, int lane, int row, i
   }
 }
 
-// The warp's 32 rows x 128 bytes of output out of shared memory, whole lines per instruction (16-byte units permuted with the row:
-// conflict-free both ways); ragged chunks and rows that do not start on 16 bytes an element per lane.
+// The warp's 32 rows x 128 bytes of output out of shared memory (16-byte units permuted with the row) an element per lane: where
+// rows do not start on 16 bytes.  Others go out by bulk copies, which the epilogue does not wait for.
 template <typename T>
-__device__ __forceinline__ void store_rows(const uint4* stage, int lane, T* out, int64_t ld, int rows, int cols, bool vec) {
-  constexpr int kCols = 128 / sizeof(T);
-  if (cols == kCols && vec) {
+__device__ __forceinline__ void store_rows(const uint4* stage, int lane, T* out, int64_t ld, int rows, int cols) {
+  constexpr int kCols = 128 / sizeof(T), kUnit = 16 / sizeof(T);
+  const T* w = reinterpret_cast<const T*>(stage);
+#pragma unroll 4
+  for (int row = 0; row < rows; ++row)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = 4 * i + (lane >> 3), u = lane & 7;
-      if (row < rows) *reinterpret_cast<uint4*>(out + row * ld + u * (16 / sizeof(T))) = stage[row * 8 + (u ^ (row & 7))];
-    }
-  } else {
-    const T* w = reinterpret_cast<const T*>(stage);
-    constexpr int kUnit = 16 / sizeof(T);
-    for (int row = 0; row < rows; ++row)
-#pragma unroll
-      for (int c = lane; c < kCols; c += 32)
-        if (c < cols) out[row * ld + c] = w[row * kCols + ((c / kUnit) ^ (row & 7)) * kUnit + c % kUnit];
-  }
+    for (int c = lane; c < kCols; c += 32)
+      if (c < cols) out[row * ld + c] = w[row * kCols + ((c / kUnit) ^ (row & 7)) * kUnit + c % kUnit];
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1)
+               : "memory");
 }
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
-                   const __grid_constant__ CUtensorMap map_u, const ManyArgs a) {
+                   const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_out, const ManyArgs a) {
   constexpr bool GATED = ACT != kNoAct;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  SharedMany* sh = reinterpret_cast<SharedMany*>(tiles + (size_t)kManyStages * kManyStageBytes);
+  uint8_t* const staging = tiles + (size_t)kManyStages * kManyStageBytes;
+  SharedMany* sh = reinterpret_cast<SharedMany*>(staging + kEpiWarps * kOutBytes);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
   const Waiter w{&sh->abort_flag, nullptr, a.waits.limit_ns};
   constexpr int kTileN = GATED ? 128 : 256;                                   // output columns of a tile
 
-  if (warp == 0 && lane < 2 + (int)GATED) {
-    const CUtensorMap* maps[3] = {&map_x, &map_w, &map_u};
+  if (warp == 0 && lane < 4) {
+    const CUtensorMap* maps[4] = {&map_x, &map_w, &map_u, &map_out};
     asm volatile("prefetch.tensormap [%0];" ::"l"(maps[lane]) : "memory");
   }
   if (threadIdx.x == 0) {
@@ -508,7 +511,7 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
   } else {
     // epilogue, warps 2..9 of both CTAs; the two warps of a lane quarter (32 rows of x) take half of the columns each
     const int q = warp & 3, h = (warp - 2) >> 2, et = (int)threadIdx.x - 64;
-    uint4* const stage = sh->stage[warp - 2];
+    uint4* const stage = reinterpret_cast<uint4*>(staging + (warp - 2) * kOutBytes);
     T* const out = static_cast<T*>(a.out);
     constexpr int kChunk = 128 / sizeof(T);
     const bool has_bias = a.sc.bias != nullptr;
@@ -547,6 +550,10 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       for (int c = h * (kTileN / 2); c < (h + 1) * (kTileN / 2); c += kChunk) {
         if (c0 + c >= a.N) break;                                             // uniform across the warp
         const int cols = (int)(a.N - c0 - c < kChunk ? a.N - c0 - c : kChunk);
+        if (a.vec) {                                                          // the last copy has read the buffer
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
+        }
 #pragma unroll
         for (int part = 0; part < kChunk; part += 32) {
           uint32_t r[2][16], u[2][16];
@@ -585,14 +592,24 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             stage_16x32(smem_u32(stage), lane, 16 * hf, part, y, T());
           }
         }
-        __syncwarp();
-        store_rows<T>(stage, lane, out + row0 * a.ld + c0 + c, a.ld, rows, cols, a.vec);
-        __syncwarp();
+        if (a.vec) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (rows > 0) tma_store_2d(&map_out, smem_u32(stage), (int)c0 + c, (int)row0);      // clipped to M x N
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else {
+          __syncwarp();
+          store_rows<T>(stage, lane, out + row0 * a.ld + c0 + c, a.ld, rows, cols);
+          __syncwarp();
+        }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->tmem_empty[buf]), 0));
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
 
   tc_fence_before();
@@ -633,9 +650,20 @@ bool code_map(CUtensorMap* m, const uint8_t* base, int64_t K, int64_t rows, int6
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename K, typename A>
+// The output: boxes of 32 rows of 128 bytes.
+bool out_map(CUtensorMap* m, void* base, int dtype, int64_t M, int64_t N, int64_t ld) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const bool bf16 = dtype == QM_DT_BF16;
+  const cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)M}, strides[1] = {(cuuint64_t)ld * (bf16 ? 2 : 4)};
+  const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32u}, step[2] = {1, 1};
+  return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, step,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename K, typename... P>
 qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t smem_most, unsigned grid, unsigned cluster,
-                         const CUtensorMap (&maps)[3], const A& a, cudaStream_t s) {
+                         cudaStream_t s, const P&... params) {
   const int dev = current_device();
   if (dev < 0) return QM_ERR_UNSUPPORTED;
   if (!ready[dev]) {
@@ -650,7 +678,7 @@ qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at; cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  QM_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], a));
+  QM_CUDA_OK(cudaLaunchKernelEx(&cfg, kern, params...));
   count_launch();
   return QM_OK;
 }
@@ -680,7 +708,9 @@ qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
   const size_t stage = (GATED ? 2 : 1) * kBlockBytes + (size_t)a.nt * kBlock;
   a.stages = (int)std::min<size_t>(kFewStages, kFewRing / stage);
   if(e_st) a.stages=std::min(e_st,a.stages);
-  a.sums_bytes = a.split > 1 ? (uint32_t)((GATED ? 2 : 1) * (a.nt + a.split - 1) * kBlock * 4) : 0u;
+  const int own = (int)((std::min<int64_t>(l.M, a.nt) + a.split - 1) / a.split);
+  while ((1 << a.own_log2) < own) ++a.own_log2;
+  a.sums_bytes = a.split > 1 ? (uint32_t)((GATED ? 2 : 1) * a.split << a.own_log2) * kBlock * 4 : 0u;
   a.stages = std::min(a.stages, (a.num_kb + a.split - 1) / a.split);
   while (a.stages*stage+a.sums_bytes > kFewRing) --a.stages;
   a.tiles_m = (int)tiles_m;
@@ -694,14 +724,14 @@ qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
   return launch_cluster(linear_few_kernel<T, ACT>, ready, 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), kFewSmem,
-                        (unsigned)(tiles * a.split), (unsigned)a.split, maps, a, s);
+                        (unsigned)(tiles * a.split), (unsigned)a.split, s, maps[0], maps[1], maps[2], a);
 }
 
 template <typename T, int ACT>
 qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   constexpr bool GATED = ACT != kNoAct;
   static bool ready[kMaxDevices] = {};
-  constexpr size_t smem = 1024 + (size_t)kManyStages * kManyStageBytes + sizeof(SharedMany);
+  constexpr size_t smem = 1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + sizeof(SharedMany);
   static_assert(smem <= 232448, "shared memory of a CTA");
   ManyArgs a{};
   a.M = l.M; a.N = l.N;
@@ -713,12 +743,15 @@ qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   a.sc = scales_of(l); a.out = l.out; a.ld = l.ld_out;
   a.vec = (reinterpret_cast<uintptr_t>(l.out) & 15) == 0 && (l.ld_out * sizeof(T)) % 16 == 0;
   wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
-  CUtensorMap maps[3];
+  CUtensorMap maps[4];
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, kBlock) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
+  if (!a.vec) maps[3] = maps[0];                                              // not used
+  else if (!out_map(&maps[3], l.out, l.out_dtype, l.M, l.N, l.ld_out)) return QM_ERR_CUDA;
   const int pairs = sm_count() / 2;
-  return launch_cluster(linear_many_kernel<T, ACT>, ready, smem, smem, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 2u, maps, a, s);
+  return launch_cluster(linear_many_kernel<T, ACT>, ready, smem, smem, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 2u, s, maps[0], maps[1], maps[2],
+                        maps[3], a);
 }
 
 template <typename T, int ACT>
