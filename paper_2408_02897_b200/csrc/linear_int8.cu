@@ -15,8 +15,6 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
-#include <cstdio>
-#include <cstdlib>
 
 #include "qm_internal.h"
 #include "tc_ptx.cuh"
@@ -397,12 +395,12 @@ __device__ __forceinline__ void stage_16x32(uint32_t stage, int lane, int row, i
   }
 }
 
-// The warp's 32 rows x 128 bytes of output out of shared memory (16-byte units permuted with the row) an element per lane: where
-// rows do not start on 16 bytes.  Others go out by bulk copies, which the epilogue does not wait for.
-template <typename T>
-__device__ __forceinline__ void store_rows(const uint4* stage, int lane, T* out, int64_t ld, int rows, int cols) {
-  constexpr int kCols = 128 / sizeof(T), kUnit = 16 / sizeof(T);
-  const T* w = reinterpret_cast<const T*>(stage);
+// The warp's 32 rows x 128 bytes of output out of shared memory (16-byte units permuted with the row) a word or, where rows start on
+// two bytes, an element per lane: for rows that do not start on 16 bytes.  Others go out by bulk copies, which the epilogue does not wait for.
+template <typename W>
+__device__ __forceinline__ void store_rows(const uint4* stage, int lane, W* out, int64_t ld, int rows, int cols) {
+  constexpr int kCols = 128 / sizeof(W), kUnit = 16 / sizeof(W);
+  const W* w = reinterpret_cast<const W*>(stage);
 #pragma unroll 4
   for (int row = 0; row < rows; ++row)
 #pragma unroll
@@ -601,7 +599,13 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           }
         } else {
           __syncwarp();
-          store_rows<T>(stage, lane, out + row0 * a.ld + c0 + c, a.ld, rows, cols);
+          T* const to = out + row0 * a.ld + c0 + c;
+          if (sizeof(T) == 2 && ((reinterpret_cast<uintptr_t>(to) & 3) | (a.ld & 1)) == 0) {
+            store_rows(stage, lane, reinterpret_cast<uint32_t*>(to), a.ld >> 1, rows, cols >> 1);
+            if ((cols & 1) && lane < rows) to[lane * a.ld + cols - 1] = reinterpret_cast<const T*>(stage)[lane * kChunk + (((cols - 1) / 8) ^ (lane & 7)) * 8 + (cols - 1) % 8];
+          } else {
+            store_rows(stage, lane, to, a.ld, rows, cols);
+          }
           __syncwarp();
         }
       }
@@ -683,36 +687,62 @@ qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t
   return QM_OK;
 }
 
+bool rows_on_16(const LinearArgs& l) {
+  return (reinterpret_cast<uintptr_t>(l.out) & 15) == 0 && l.ld_out * (l.out_dtype == QM_DT_BF16 ? 2 : 4) % 16 == 0;
+}
+
 Scales scales_of(const LinearArgs& l) {
   return {l.dx, {l.dw[0], l.dw[1]}, l.bias, l.bias_dtype == QM_DT_BF16};
+}
+
+// Which kernel, and how the few rows' one is cut, by the time that it takes: rows of x per tile (nt), parts of the contraction (split),
+// in ns by what was measured on 148 SMs at 1 to 1024 rows, 1024 to 8192 weight rows and contractions of 1024 to 8192:
+//   a CTA of the few rows' kernel: kBase, kDepth for each 128 contraction entries (the MMA warp's issue, not the tensor cores, so that more
+//   rows cost little), kSplit where sums are exchanged; as often as the CTAs, one to an SM, fill the GPU;
+//   the many rows' kernel: 5000, and for each round of its tiles 310 for 128 contraction entries or the epilogue's 2500, 5500 where the
+//   output's rows do not start on 16 bytes.
+// What it settles (us, product of 4096 x 4096 weights): 64 rows (nt 64, split 4) 6.6, (64, 1) 9.5, many 13.3; 256 rows (128, 2) 10.0,
+// (64, 2) 16.2, many 13.7; 1024 rows many 15.5, (128, 1) 22.6.
+struct Plan { int nt, split; };            // nt 0: the many rows' kernel
+Plan make_plan(const LinearArgs& l, bool gated, bool aligned) {
+  static constexpr int kNt[4] = {16, 32, 64, 128};
+  static constexpr int64_t kBase[2][4] = {{2200, 2500, 3100, 4100}, {2300, 2800, 3700, 4700}};
+  static constexpr int64_t kDepth[2][4] = {{200, 200, 205, 225}, {300, 310, 330, 390}};
+  static constexpr int64_t kSplit[2][4] = {{600, 800, 1100, 2200}, {800, 1000, 1700, 6000}};
+  const int64_t sms = sm_count(), num_kb = (l.K + kBlock - 1) / kBlock, tiles_n = (l.N + kBlock - 1) / kBlock;
+  const int64_t pairs = sms / 2, tiles = (l.M + 255) / 256 * ((l.N + (gated ? 127 : 255)) / (gated ? 128 : 256));
+  int64_t best = 5000 + (tiles + pairs - 1) / pairs * std::max<int64_t>(310 * num_kb, aligned ? 2500 : 5500);
+  Plan plan{0, 1};
+  for (int i = 0; i < 4 && (i == 0 || kNt[i - 1] < l.M); ++i) {
+    const int64_t ctas = tiles_n * ((l.M + kNt[i] - 1) / kNt[i]);
+    if (ctas > 64 * sms) continue;
+    // (a cluster lies inside one of the GPU's eight groups of SMs, so not every SM is in one of four or eight)
+    for (int split = 1; split <= kMaxSplit && split <= num_kb && (split == 1 || ctas * split <= sms - 4 * split); split *= 2) {
+      const int64_t one = kBase[gated][i] + (num_kb + split - 1) / split * kDepth[gated][i] + (split > 1 ? kSplit[gated][i] + 50 * split : 0);
+      const int64_t t = 900 + (ctas * split + sms - 1) / sms * (one - 900);
+      if (t < best) { best = t; plan = {kNt[i], split}; }
+    }
+  }
+  return plan;
 }
 
 constexpr size_t kFewRing = 200 * 1024;
 constexpr size_t kFewSmem = 1024 + kFewRing + sizeof(SharedFew);
 
 template <typename T, int ACT>
-qm_status launch_few(const LinearArgs& l, cudaStream_t s) {
+qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   constexpr bool GATED = ACT != kNoAct;
   static bool ready[kMaxDevices] = {};
   FewArgs a{};
   a.M = l.M; a.N = l.N;
   a.num_kb = (int)((l.K + kBlock - 1) / kBlock);
-  int e_nt=0,e_split=0,e_st=0; if(const char*e=getenv("QM_FEW")) sscanf(e,"%d,%d,%d",&e_nt,&e_split,&e_st);
-  a.nt = 16;
-  while (a.nt < 128 && a.nt < l.M) a.nt *= 2;
-  if(e_nt) a.nt=e_nt;
+  a.nt = plan.nt; a.split = plan.split;
   const int64_t tiles_m = (l.M + a.nt - 1) / a.nt, tiles = (l.N + kBlock - 1) / kBlock * tiles_m;
-  a.split = 1;
-  while (a.split < kMaxSplit && 2 * a.split <= a.num_kb && tiles * 2 * a.split <= sm_count()) a.split *= 2;
-  if(e_split) a.split=std::min(e_split,a.num_kb);
   const size_t stage = (GATED ? 2 : 1) * kBlockBytes + (size_t)a.nt * kBlock;
-  a.stages = (int)std::min<size_t>(kFewStages, kFewRing / stage);
-  if(e_st) a.stages=std::min(e_st,a.stages);
   const int own = (int)((std::min<int64_t>(l.M, a.nt) + a.split - 1) / a.split);
   while ((1 << a.own_log2) < own) ++a.own_log2;
   a.sums_bytes = a.split > 1 ? (uint32_t)((GATED ? 2 : 1) * a.split << a.own_log2) * kBlock * 4 : 0u;
-  a.stages = std::min(a.stages, (a.num_kb + a.split - 1) / a.split);
-  while (a.stages*stage+a.sums_bytes > kFewRing) --a.stages;
+  a.stages = (int)std::min<size_t>({(size_t)kFewStages, (kFewRing - a.sums_bytes) / stage, (size_t)((a.num_kb + a.split - 1) / a.split)});
   a.tiles_m = (int)tiles_m;
   a.idesc = make_idesc(2, 1, 1, kBlock, (uint32_t)a.nt);                      // s8 x s8 -> s32
   a.tmem_cols = std::max(32, a.nt * (GATED ? 2 : 1));
@@ -741,7 +771,7 @@ qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   if (tiles >= (1ll << 31) - 1024) return QM_ERR_UNSUPPORTED;                 // the walk adds the grid to an index
   a.num_tiles = (int)tiles;
   a.sc = scales_of(l); a.out = l.out; a.ld = l.ld_out;
-  a.vec = (reinterpret_cast<uintptr_t>(l.out) & 15) == 0 && (l.ld_out * sizeof(T)) % 16 == 0;
+  a.vec = rows_on_16(l);
   wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
   CUtensorMap maps[4];
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, kBlock) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
@@ -756,8 +786,8 @@ qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
 
 template <typename T, int ACT>
 qm_status launch_sized(const LinearArgs& l, cudaStream_t s) {
-  int few = l.M <= 512; if(const char*e=getenv("QM_KIND")) few = atoi(e);
-  return few ? launch_few<T, ACT>(l, s) : launch_many<T, ACT>(l, s);
+  const Plan plan = make_plan(l, ACT != kNoAct, rows_on_16(l));
+  return plan.nt ? launch_few<T, ACT>(l, plan, s) : launch_many<T, ACT>(l, s);
 }
 
 template <typename T>
