@@ -271,15 +271,14 @@ def _refuse(why):
 
 def _matrix(t, what, dtypes, device):
     """(rows, cols, pitch) of a 2-D tensor, or a 3-D one with one batch element, whose rows are contiguous."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 3 and shape[0] == 1:
-        shape, stride = shape[1:], stride[1:]
-    if len(shape) != 2 or t.dtype not in dtypes or t.get_device() != device:
+    dims = t.dim()
+    if (dims != 2 and (dims != 3 or t.shape[0] != 1)) or t.dtype not in dtypes or t.get_device() != device:
         _refuse(f"{what}: wants a 2-D {' or '.join(map(str, dtypes))} tensor on the current CUDA device")
-    rows, cols = shape
-    if stride[1] != 1 and cols > 1:
+    rows, cols = t.shape[-2:]
+    pitch, unit = t.stride()[-2:]
+    if unit != 1 and cols > 1:
         _refuse(f"{what}: the elements of a row must be contiguous")
-    return rows, cols, stride[0] if rows > 1 else cols
+    return rows, cols, pitch if rows > 1 else cols
 
 
 def _vector(t, what, n, dtypes, device):
@@ -326,10 +325,11 @@ def qm_rms_norm_quantize(x, weight, eps, fmt, residual=None, residual_out=None, 
     r = z = None
     ld_r = ld_z = 0
     if residual is not None:
-        if residual_out is None:
-            residual_out = _new(x, (rows, cols), dt, stream)
         r_rows, r_cols, ld_r = _matrix(residual, "residual", (dt,), device)
-        z_rows, z_cols, ld_z = _matrix(residual_out, "residual_out", (dt,), device)
+        if residual_out is None:
+            residual_out, z_rows, z_cols, ld_z = _new(x, (rows, cols), dt, stream), rows, cols, cols
+        else:
+            z_rows, z_cols, ld_z = _matrix(residual_out, "residual_out", (dt,), device)
         if not r_rows == z_rows == rows or not r_cols == z_cols == cols:
             _refuse("x, residual and residual_out differ in shape")
         r, z = residual.data_ptr(), residual_out.data_ptr()
