@@ -699,19 +699,19 @@ Scales scales_of(const LinearArgs& l) {
 // in ns by what was measured on 148 SMs at 1 to 1024 rows, 1024 to 8192 weight rows and contractions of 1024 to 8192:
 //   a CTA of the few rows' kernel: kBase, kDepth for each 128 contraction entries (the MMA warp's issue, not the tensor cores, so that more
 //   rows cost little), kSplit where sums are exchanged; as often as the CTAs, one to an SM, fill the GPU;
-//   the many rows' kernel: 5000, and for each round of its tiles 310 for 128 contraction entries or the epilogue's 2500, 5500 where the
-//   output's rows do not start on 16 bytes.
+//   the many rows' kernel: 5000, and for each round of its tiles 310 for 128 contraction entries or the epilogue's 2500, where the output's
+//   rows do not start on 16 bytes 5000 in bf16, 6000 in fp32 and 3600 of the gated form's narrower tiles.
 // What it settles (us, product of 4096 x 4096 weights): 64 rows (nt 64, split 4) 6.6, (64, 1) 9.5, many 13.3; 256 rows (128, 2) 10.0,
 // (64, 2) 16.2, many 13.7; 1024 rows many 15.5, (128, 1) 22.6.
 struct Plan { int nt, split; };            // nt 0: the many rows' kernel
 Plan make_plan(const LinearArgs& l, bool gated, bool aligned) {
   static constexpr int kNt[4] = {16, 32, 64, 128};
-  static constexpr int64_t kBase[2][4] = {{2200, 2500, 3100, 4100}, {2300, 2800, 3700, 4700}};
+  static constexpr int64_t kBase[2][4] = {{2200, 2500, 3100, 4100}, {2300, 2800, 3700, 5200}};
   static constexpr int64_t kDepth[2][4] = {{200, 200, 205, 225}, {300, 310, 330, 390}};
   static constexpr int64_t kSplit[2][4] = {{600, 800, 1100, 2200}, {800, 1000, 1700, 6000}};
   const int64_t sms = sm_count(), num_kb = (l.K + kBlock - 1) / kBlock, tiles_n = (l.N + kBlock - 1) / kBlock;
   const int64_t pairs = sms / 2, tiles = (l.M + 255) / 256 * ((l.N + (gated ? 127 : 255)) / (gated ? 128 : 256));
-  int64_t best = 5000 + (tiles + pairs - 1) / pairs * std::max<int64_t>(310 * num_kb, aligned ? 2500 : 5500);
+  int64_t best = 5000 + (tiles + pairs - 1) / pairs * std::max<int64_t>(310 * num_kb, aligned ? 2500 : gated ? 3600 : l.out_dtype == QM_DT_BF16 ? 5000 : 6000);
   Plan plan{0, 1};
   for (int i = 0; i < 4 && (i == 0 || kNt[i - 1] < l.M); ++i) {
     const int64_t ctas = tiles_n * ((l.M + kNt[i] - 1) / kNt[i]);
@@ -753,7 +753,9 @@ qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, a.nt) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
-  return launch_cluster(linear_few_kernel<T, ACT>, ready, 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), kFewSmem,
+  // Tensor memory's columns are waited for: CTAs of one SM never ask for more than there are, whatever their registers leave room for.
+  const size_t smem = std::max<size_t>(1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), (size_t)232448 * a.tmem_cols / 512);
+  return launch_cluster(linear_few_kernel<T, ACT>, ready, smem, kFewSmem,
                         (unsigned)(tiles * a.split), (unsigned)a.split, s, maps[0], maps[1], maps[2], a);
 }
 

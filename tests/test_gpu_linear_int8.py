@@ -100,6 +100,31 @@ def test_gated(M, N, K, act):
     within(h, want, tol, act)
 
 
+# A shape for each way in which the products are cut on 148 SMs (rows of x per tile and parts of the contraction; then tiles of CTA pairs,
+# several to a pair, in outputs whose rows start on 16, 8, 4 and 2 bytes)
+CUTS = [(1, 4450, 907), (1, 65, 782), (1, 65, 1552), (17, 9483, 16), (18, 4509, 1708), (569, 129, 1435), (261, 129, 1801), (257, 135, 1400),
+        (237, 65, 3597), (2475, 131, 16), (1240, 130, 2525), (593, 129, 2919), (559, 67, 5833), (265, 135, 6829), (67, 9615, 16),
+        (2547, 135, 4553), (2251, 69, 5896), (2398, 135, 7447),
+        (3333, 2600, 144), (3333, 2604, 144), (3333, 2603, 144), (6000, 2050, 1000), (6001, 2051, 1000), (411, 9936, 16)]
+
+
+@pytest.mark.parametrize("M,N,K", CUTS)
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_every_cut(M, N, K, dt):
+    cx, x = codes(M, K, 50)
+    cw, w = codes(N, K, 51)
+    cu, up = codes(N, K, 52)
+    std = 127 * 127 / 3 * np.sqrt(K)
+    dx, dw, du = deltas(M, 53, 0.01), deltas(N, 54, 300.0 / std), deltas(N, 55, 100.0 / std)
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(56))
+    g = layer.product_int8(cx, dx.numpy(), cw, dw.numpy())
+    u = layer.product_int8(cx, dx.numpy(), cu, du.numpy())
+    want = g + bias.double().numpy()[None, :]
+    within(qm.qm_linear_int8(x, dx.cuda(), w, dw.cuda(), K, bias=bias.cuda(), out_dtype=dt), want, linear_tolerance(g, want, dt), "linear")
+    want, tol = gated_reference(g, u, "silu", dt)
+    within(qm.qm_gated_linear_int8(x, dx.cuda(), w, dw.cuda(), up, du.cuda(), K, act="silu", out_dtype=dt), want, tol, "gated")
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("M", [3, 300])
 def test_gated_far_out(act, M):

@@ -61,6 +61,20 @@ def test_against_oracle(rows, cols, dtype, fmt):
     check(x, w, 1e-5, fmt, None, qm.qm_rms_norm_quantize(x, w, 1e-5, fmt))
 
 
+# more rows than SMs (several to a block), a length for each shape of the kernel, rows that start on 16 bytes and rows that do not
+@pytest.mark.parametrize("rows,cols", [(1500, 200), (1700, 513), (900, 1000), (900, 1001), (700, 1530), (701, 2041), (640, 3000), (650, 3001), (600, 4088),
+                                       (610, 4095), (400, 6000), (400, 8185), (300, 12001), (200, 16384)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_more_rows_than_are_held_at_once(rows, cols, dtype, fmt):
+    x, r = make(rows, cols, dtype, 20), make(rows, cols, dtype, 21, spread=3.0)
+    w = (1 + 0.1 * torch.randn(cols, generator=torch.Generator().manual_seed(22))).to(DT[dtype]).cuda()
+    check(x, w, 1e-6, fmt, r, qm.qm_rms_norm_quantize(x, w, 1e-6, fmt, residual=r))
+    check(x, w, 1e-6, fmt, None, qm.qm_rms_norm_quantize(x, w, 1e-6, fmt))
+    z = r.clone()                                                    # in place, every row ahead of its own writing
+    check(x, w, 1e-6, fmt, r, qm.qm_rms_norm_quantize(x, w, 1e-6, fmt, residual=z, residual_out=z))
+
+
 @pytest.mark.parametrize("rows,cols,pad,lead", [(5, 64, 8, 8), (5, 64, 8, 0), (4, 1024, 16, 16), (7, 1024, 3, 1), (3, 1000, 8, 8),
                                                 (6, 999, 1, 1), (2, 4096, 64, 2), (3, 5000, 5, 4)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
