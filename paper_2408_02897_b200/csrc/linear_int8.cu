@@ -79,6 +79,7 @@ struct FewArgs {
   int64_t M, N;
   int num_kb, tiles_m, split, nt, stages;    // nt: rows of x per tile, 16 .. 128
   uint32_t sums_bytes;
+  int prefetch;                              // weight blocks asked into L2 ahead of the kernel before this one
   int own_log2;                              // of a split contraction, rows of x that a CTA of the cluster finishes
   uint32_t idesc, tmem_cols;
   Scales sc;
@@ -116,7 +117,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&y)[4], in
 }
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                   const __grid_constant__ CUtensorMap map_u, const FewArgs a) {
   constexpr bool GATED = ACT != kNoAct;
@@ -156,7 +157,14 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   tc_fence_before();
   __syncthreads();
   if (a.split > 1) cluster_arrive();               // this CTA's shared memory may be written by its peers
-  pdl_prologue();
+  // The next kernel in the stream is let in when this one's loads are all on their way, so that its set-up runs under the epilogue here.
+  // What it may do ahead of its wait is a prefetch into L2, which a later write cannot make stale: of large weights the first blocks.
+  if (a.prefetch && warp == 0 && lane == 0)
+    for (int k = 0; k < a.prefetch && kb0 + k < kb1; ++k) {
+      prefetch_2d(&map_w, (kb0 + k) * kBlock, n0);
+      if (GATED) prefetch_2d(&map_u, (kb0 + k) * kBlock, n0);
+    }
+  pdl_wait();
   tc_fence_after();
   const uint32_t tmem_base = sh->tmem_base;
 
@@ -176,6 +184,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         if (++s == a.stages) { s = 0; parity ^= 1u; }
       }
       sh->issued = g;
+      pdl_launch_dependents();
     }
   } else if (warp == 1) {
     const bool lead = elect_one();
@@ -742,7 +751,14 @@ qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   const int own = (int)((std::min<int64_t>(l.M, a.nt) + a.split - 1) / a.split);
   while ((1 << a.own_log2) < own) ++a.own_log2;
   a.sums_bytes = a.split > 1 ? (uint32_t)((GATED ? 2 : 1) * a.split << a.own_log2) * kBlock * 4 : 0u;
-  a.stages = (int)std::min<size_t>({(size_t)kFewStages, (kFewRing - a.sums_bytes) / stage, (size_t)((a.num_kb + a.split - 1) / a.split)});
+  // A part of the contraction that is on its way at once anyhow gets half an SM's shared memory, so that the next kernel's CTAs find room
+  // beside it (1 x 4096 x 4096 5.3 -> 4.5 us); longer ones get it all: CTAs of one kernel two to an SM leave others without (64 x 8192 x
+  // 8192 14.7 us, 23 in half rings).
+  const size_t blocks = (size_t)((a.num_kb + a.split - 1) / a.split), ring = blocks * stage;
+  const bool shortly = ring <= 160 * 1024;
+  a.stages = (int)std::min<size_t>({(size_t)kFewStages, blocks, (shortly ? kFewRing / 2 - std::min<size_t>(a.sums_bytes, kFewRing / 4) : kFewRing - a.sums_bytes) / stage});
+  // weights that do not stay in L2 between calls: 24 x 8192 x 4096 gated 14.4 -> 13.9 us; smaller ones lose up to 1 us by it
+  a.prefetch = (GATED ? 2 : 1) * l.N * l.K >= (32ll << 20) ? 4 : 0;
   a.tiles_m = (int)tiles_m;
   a.idesc = make_idesc(2, 1, 1, kBlock, (uint32_t)a.nt);                      // s8 x s8 -> s32
   a.tmem_cols = std::max(32, a.nt * (GATED ? 2 : 1));

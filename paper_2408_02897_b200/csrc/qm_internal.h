@@ -46,9 +46,11 @@ int sm_count();         // of the current device
 // launch gap between the short dependent kernels of a probe.
 bool pdl_enabled();   // on unless the environment has QM_PDL=0
 #ifdef __CUDACC__
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_prologue() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  pdl_wait();
+  pdl_launch_dependents();
 }
 // The two halves of a barrier over the cluster's threads.  The aligned form wants a warp's threads together, which after a branch that
 // some of them took only __syncwarp() promises.

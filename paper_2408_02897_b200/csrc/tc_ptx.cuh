@@ -258,6 +258,10 @@ __device__ __forceinline__ void tma_load_2d_local(uint32_t dst, const CUtensorMa
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1)
       : "memory");
 }
+// Such a tile's bytes into L2, nothing else.
+__device__ __forceinline__ void prefetch_2d(const CUtensorMap* map, int c0, int c1) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(c0), "r"(c1) : "memory");
+}
 // The same for the CTA pair's MMAs: the byte count goes to the barrier at `bar_cluster_addr`, in either CTA.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int c0, int c1) {
   asm volatile(
