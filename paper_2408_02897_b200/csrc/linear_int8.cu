@@ -72,6 +72,13 @@ __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
   return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
 }
 
+// A wait of the give-up path, whatever the CTA has been flagged with.
+__device__ __forceinline__ void wait_limited(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait(bar, parity) && global_timer_ns() - t0 < limit_ns) {}
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 
 // ------------------------------------------------------------------ few rows
@@ -90,8 +97,8 @@ struct FewArgs {
 constexpr int kFewStages = 12;
 constexpr int kMaxSplit = 8;
 struct SharedFew {
-  uint64_t full[kFewStages], empty[kFewStages], done, drain;
-  uint32_t tmem_base, abort_flag, issued, gave_up;     // gave_up: some CTA of the cluster did
+  uint64_t full[kFewStages], empty[kFewStages], done, drain, read;
+  uint32_t tmem_base, abort_flag, gave_up, pad;        // gave_up: some CTA of the cluster did
   float dx[256];
 };
 
@@ -145,10 +152,15 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     }
     mbar_init(smem_u32(&sh->done), 1);
     mbar_init(smem_u32(&sh->drain), 1);
-    sh->abort_flag = 0; sh->issued = 0; sh->gave_up = 0;
+    mbar_init(smem_u32(&sh->read), kEpiWarps);
+    sh->abort_flag = 0; sh->gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  // Tensor memory is waited for where CTAs of other kernels on this SM hold it, and a CTA that holds some must not wait for one that waits
+  // for some: a CTA tells its peers ahead of its allocation that its shared memory may be written, and gives its columns back ahead of
+  // its wait for their sums.
+  if (a.split > 1) cluster_arrive();
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(a.tmem_cols)
                  : "memory");
@@ -156,7 +168,6 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   }
   tc_fence_before();
   __syncthreads();
-  if (a.split > 1) cluster_arrive();               // this CTA's shared memory may be written by its peers
   // The next kernel in the stream is let in when this one's loads are all on their way, so that its set-up runs under the epilogue here.
   // What it may do ahead of its wait is a prefetch into L2, which a later write cannot make stale: of large weights the first blocks.
   if (a.prefetch && warp == 0 && lane == 0)
@@ -168,6 +179,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = sh->tmem_base;
 
+  uint32_t loads = 0;
   if (warp == 0) {
     if (lane == 0) {
       uint32_t g = 0;
@@ -183,9 +195,10 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         tma_load_2d_local(base + kW * kBlockBytes, &map_x, bar, kb * kBlock, m0);
         if (++s == a.stages) { s = 0; parity ^= 1u; }
       }
-      sh->issued = g;
       pdl_launch_dependents();
+      loads = g;
     }
+    if (a.split > 1) { cluster_wait(); cluster_arrive(); }
   } else if (warp == 1) {
     const bool lead = elect_one();
     int s = 0;
@@ -208,6 +221,17 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       if (++s == a.stages) { s = 0; parity ^= 1u; }
     }
     if (ok && lead) tc_commit_one(smem_u32(&sh->done));
+    // the columns back when the epilogue has read them (or given up), ahead of the wait for the peers' sums
+    if (a.split > 1) { cluster_wait(); cluster_arrive(); }
+    wait_limited(smem_u32(&sh->read), 0, a.waits.limit_ns);
+    if (sh->abort_flag) {                          // give-up path: MMAs that nobody has waited for
+      __syncwarp();
+      if (lead) tc_commit_one(smem_u32(&sh->drain));
+      wait_limited(smem_u32(&sh->drain), 0, a.waits.limit_ns);
+    }
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
   }
 
   // epilogue, warps 2..9: a warp may read the quarter warp % 4 of tensor memory's lanes; the two warps of a quarter take every
@@ -283,10 +307,13 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
       }
     }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sh->read));
+    if (a.split > 1) cluster_arrive();
   }
   if (a.split > 1) {
-    if (warp < 2) cluster_wait();
-    cluster_sync();
+    cluster_wait();
     const int cols = (int)(a.N - n0 - j < 4 ? a.N - n0 - j : 4);
     if (warp >= 2 && cols > 0) {
       const bool ok = sh->gave_up == 0;
@@ -319,29 +346,10 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       }
     }
   }
-
-  tc_fence_before();
   __syncthreads();
-  if (sh->abort_flag) {
-    // give-up path: loads and MMAs that nobody has waited for
-    if (threadIdx.x == 0) {
-      const uint32_t n = sh->issued, st = (uint32_t)a.stages;
-      for (uint32_t g = n > st ? n - st : 0u; g < n; ++g) {
-        const uint64_t t0 = global_timer_ns();
-        while (!mbar_try_wait(smem_u32(&sh->full[g % st]), (g / st) & 1) && global_timer_ns() - t0 < a.waits.limit_ns) {}
-      }
-    }
-    if (warp == 1) {
-      if (elect_one()) tc_commit_one(smem_u32(&sh->drain));
-      const uint64_t t0 = global_timer_ns();
-      while (!mbar_try_wait(smem_u32(&sh->drain), 0) && global_timer_ns() - t0 < a.waits.limit_ns) {}
-    }
-    __syncthreads();
-  }
-  if (warp == 1) {
-    __syncwarp();
-    tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
+  if (sh->abort_flag && threadIdx.x == 0) {        // give-up path: loads that nobody has waited for
+    const uint32_t st = (uint32_t)a.stages;
+    for (uint32_t g = loads > st ? loads - st : 0u; g < loads; ++g) wait_limited(smem_u32(&sh->full[g % st]), (g / st) & 1, a.waits.limit_ns);
   }
 }
 
@@ -631,16 +639,13 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     // give-up path: loads (both CTAs' complete on the leader's barriers) and MMAs that nobody has waited for
     if (threadIdx.x == 0 && rank == 0) {
       const uint32_t n = sh->issued;
-      for (uint32_t g = n > (uint32_t)kManyStages ? n - kManyStages : 0u; g < n; ++g) {
-        const uint64_t t0 = global_timer_ns();
-        while (!mbar_try_wait(smem_u32(&sh->full[g % kManyStages]), (g / kManyStages) & 1) && global_timer_ns() - t0 < a.waits.limit_ns) {}
-      }
+      for (uint32_t g = n > (uint32_t)kManyStages ? n - kManyStages : 0u; g < n; ++g)
+        wait_limited(smem_u32(&sh->full[g % kManyStages]), (g / kManyStages) & 1, a.waits.limit_ns);
     }
     if (warp == 1 && rank == 0) {
       if (elect_one())
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sh->drain)) : "memory");
-      const uint64_t t0 = global_timer_ns();
-      while (!mbar_try_wait(smem_u32(&sh->drain), 0) && global_timer_ns() - t0 < a.waits.limit_ns) {}
+      wait_limited(smem_u32(&sh->drain), 0, a.waits.limit_ns);
     }
     __syncthreads();
   }
@@ -769,8 +774,7 @@ qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, a.nt) || !code_map(&maps[1], l.w[0], l.K, l.N, l.ld_w[0], kBlock)) return QM_ERR_CUDA;
   if (!GATED) maps[2] = maps[1];
   else if (!code_map(&maps[2], l.w[1], l.K, l.N, l.ld_w[1], kBlock)) return QM_ERR_CUDA;
-  // Tensor memory's columns are waited for: CTAs of one SM never ask for more than there are, whatever their registers leave room for.
-  const size_t smem = std::max<size_t>(1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew), (size_t)232448 * a.tmem_cols / 512);
+  const size_t smem = 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew);
   return launch_cluster(linear_few_kernel<T, ACT>, ready, smem, kFewSmem,
                         (unsigned)(tiles * a.split), (unsigned)a.split, s, maps[0], maps[1], maps[2], a);
 }
@@ -779,8 +783,9 @@ template <typename T, int ACT>
 qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   constexpr bool GATED = ACT != kNoAct;
   static bool ready[kMaxDevices] = {};
-  constexpr size_t smem = 1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + sizeof(SharedMany);
-  static_assert(smem <= 232448, "shared memory of a CTA");
+  // all of an SM's shared memory: a CTA that holds tensor memory waits for its peer here, so neither may have to wait for another kernel's
+  constexpr size_t smem = 232448;
+  static_assert(1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + sizeof(SharedMany) <= smem, "shared memory of a CTA");
   ManyArgs a{};
   a.M = l.M; a.N = l.N;
   a.num_kb = (int)((l.K + kBlock - 1) / kBlock);

@@ -149,3 +149,36 @@ def test_a_freed_result_is_not_handed_out_while_its_stream_works():
     mine = [torch.empty(300, H, dtype=torch.bfloat16, device="cuda") for _ in range(64)]
     assert all(t.data_ptr() != ptr for t in mine)
     torch.cuda.synchronize()
+
+
+def test_products_beside_one_another_and_beside_probes():
+    """Kernels of several shapes on streams of their own, beside a probe and a stand-alone product, which all hold tensor memory: the
+    results are those of the calls one after the other."""
+    g = torch.Generator().manual_seed(17)
+
+    def side(rows, K):
+        c = torch.randint(-127, 128, (rows, K), generator=g, dtype=torch.int32).to(torch.int8).view(torch.uint8).cuda()
+        return c, (torch.rand(rows, generator=g) * 0.01).cuda()
+    calls = []
+    for M, N, K in ((1, 200, 1024), (3, 128, 128), (16, 1000, 4096), (70, 2000, 512), (128, 300, 2048), (600, 2048, 256), (2000, 1024, 128)):
+        x, w, u = side(M, K), side(N, K), side(N, K)
+        calls.append(lambda s, x=x, w=w, K=K: qm.qm_linear_int8(*x, *w, K, stream=s))
+        calls.append(lambda s, x=x, w=w, u=u, K=K: qm.qm_gated_linear_int8(*x, *w, *u, K, stream=s))
+        calls.append(lambda s, x=x, w=w, K=K: qm.qm_gemm(x[0][None], "int8", x[1], "channel", w[0][None], "int8", w[1], "channel", K, stream=s)[0])
+    L, R = (torch.randn(n, 512, generator=g).bfloat16().cuda() for n in (700, 900))
+    ops = (qm.operand_of(L, -1), qm.operand_of(R, -1))
+    plan = qm.ProbePlan(*ops, "int8", "int8", "tensor", "tensor")
+    want = [c(None) for c in calls]
+    plan.launch(*ops)
+    record = plan.result().record()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(6)]
+    for turn in range(8):
+        got = []
+        for i, c in enumerate(calls):
+            if i % 3 == 0:
+                plan.launch(*ops, stream=streams[0])
+            got.append(c(streams[(i + turn) % 6]))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert plan.result().record() == record
