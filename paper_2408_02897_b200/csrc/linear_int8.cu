@@ -45,7 +45,10 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return y;
 }
 
-constexpr int kNoAct = -1;       // one product; the gated kernels are compiled for each activation (see the many rows' epilogue)
+// One product.  The gated kernels are compiled for each activation: chosen in the epilogue's loop it is a branch for every output, under which no
+// other output's exponential runs (8192 x 4096 x 1024 54 us, now 50); chosen ahead of the loop, its three copies do not stay in the
+// instruction cache (63 us).
+constexpr int kNoAct = -1;
 // act(g) in fp32.
 //  GELU: g Phi(g), Phi(-|g|) = erfc(z) / 2 with z = |g| / sqrt 2 and erfc(z) = t exp(-z^2 + Q(t)), t = 1 / (1 + 0.39 z).  Q is log(erfc(z)
 //    exp(z^2) / t) interpolated at Chebyshev points for z up to 10, degree 8: 6.3e-8 off, which with fp32's roundings is 4.2 half steps of |g|
@@ -82,6 +85,14 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarri
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 
 // ------------------------------------------------------------------ few rows
+// One tile of 128 weight rows x nt rows of x per CTA, or per cluster that splits the contraction.  Roles: warp 0 issues TMA loads into a
+// ring, warp 1 holds tensor memory and issues the MMAs (weights as M, x as N), warps 2..9 are the epilogue.
+// Bound by what reaches an SM from L2, about 64 bytes a clock (18 KB for 128 contraction entries of 16 rows, 32 KB for 128), and where the
+// weights come from HBM by that: 64 x 8192 x 8192 streams its 67 MB in 9.2 of 14.2 us, 7.3 TB/s.  The rest, and most of a small
+// call (1 x 4096 x 1024 3.1 us): 0.5 to 1.5 us to the first block, 0.2 from the last block to complete accumulators, 0.6 to hand the
+// sums over, 0.4 for the cluster's barrier, 0.2 to 0.8 to finish the rows, 0.3 for the next kernel to start.  Tried: sums read
+// from the peers instead of pushed (+0.7 us), the barrier of the next block asked ahead of this block's MMAs (no
+// difference), half the ring and two CTAs to an SM for long parts (64 x 8192 x 8192 23 us: CTAs of one launch share SMs while others idle).
 struct FewArgs {
   int64_t M, N;
   int num_kb, tiles_m, split, nt, stages;    // nt: rows of x per tile, 16 .. 128
@@ -354,6 +365,13 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 }
 
 // ------------------------------------------------------------------ many rows
+// Persistent CTA pairs on tiles of 256 rows of x and 256 weight rows (gated: 128 rows of either weight), a stage of 32 KB a CTA for 128
+// contraction entries, five stages, two accumulator buffers, so that a tile's epilogue runs under the next one's MMAs.
+// Bound by the tensor cores from contractions of 2048 on (8192 x 8192 x 4096 167 us, 3.3 POP/s; 531 cycles for 128 entries, 512 at the
+// pipe's peak), below that by the output: 16384 x 4096 x 1024 takes 54 us, 44 without its stores, and 35 with a contraction
+// of 128, which is what a fill of those 134 MB takes (34.8).  Bulk stores of the staged rows and plain ones measured the same; four stages
+// 59, cache hints on the stores 53 to 54.  The gated form's epilogue alone (contraction of 128) is 39 us for 8192 x 4096 outputs, half
+// of it the activation, under 44 of MMAs.
 struct ManyArgs {
   int64_t M, N;
   int num_kb, tiles_n, num_tiles;              // tiles of 256 rows of x and 256 weight rows (gated: 128 of each weight)
