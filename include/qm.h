@@ -299,8 +299,8 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
  *  weight     `cols` values, bf16 or fp32 (`weight_dtype`).
  *  eps        positive and normal in fp32.
  *  codes      [rows][qm_code_ld(cols)], 16-byte aligned, padding zero;  delta [rows] fp32.
- * A row whose v is all zero gets delta = 1.  A NaN or Inf in x, residual or (where z is not zero) the products, or a sum
- * of squares beyond fp32, makes the row's delta NaN and its codes 0; other rows are as they would be without it.
+ * A row whose v is all zero gets delta = 1.  A row with a NaN or Inf in z or v (0 times an Inf among the weights is one), or whose sum
+ * of squares leaves fp32, gets delta = NaN and codes 0; other rows are as they would be without it.
  */
 qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int32_t dtype,
                                const void* weight, int32_t weight_dtype, float eps, int64_t rows, int64_t cols,
@@ -314,7 +314,8 @@ qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual
  *  codes_w    [N] rows of K codes, ld_w bytes apart;        delta_w [N], a scale per output channel
  *             (both 16-byte aligned, pitches multiples of 16, e.g. qm_code_ld(K); bytes from K on are not looked at)
  *  bias       optional (NULL), N values of bias_dtype (qm_dtype)
- *  out        [M] rows of N values of out_dtype (qm_dtype), ld_out elements apart; what lies between the rows stays
+ *  out        [M] rows of N values of out_dtype (qm_dtype), ld_out elements apart, apart from the inputs; what lies between
+ *             the rows stays as it was
  * A NaN scale gives NaN in its row or column.  Results do not depend on M or on how the work is split.
  * A wait inside the kernel that runs into its time limit leaves NaN in the outputs it could not compute.
  */

@@ -271,14 +271,17 @@ def _refuse(why):
 
 def _matrix(t, what, dtypes, device):
     """(rows, cols, pitch) of a 2-D tensor, or a 3-D one with one batch element, whose rows are contiguous."""
-    dims = t.dim()
-    if (dims != 2 and (dims != 3 or t.shape[0] != 1)) or t.dtype not in dtypes or t.get_device() != device:
-        _refuse(f"{what}: wants a 2-D {' or '.join(map(str, dtypes))} tensor on the current CUDA device")
-    rows, cols = t.shape[-2:]
-    pitch, unit = t.stride()[-2:]
-    if unit != 1 and cols > 1:
-        _refuse(f"{what}: the elements of a row must be contiguous")
-    return rows, cols, pitch if rows > 1 else cols
+    if t.dtype in dtypes and t.get_device() == device:
+        batch, dims = 1, t.dim()
+        if dims == 2:
+            (rows, cols), (pitch, unit) = t.shape, t.stride()
+        elif dims == 3:
+            (batch, rows, cols), (_, pitch, unit) = t.shape, t.stride()
+        if batch == 1 and 2 <= dims <= 3:
+            if unit != 1 and cols > 1:
+                _refuse(f"{what}: the elements of a row must be contiguous")
+            return rows, cols, pitch if rows > 1 else cols
+    _refuse(f"{what}: wants a 2-D {' or '.join(map(str, dtypes))} tensor on the current CUDA device")
 
 
 def _vector(t, what, n, dtypes, device):

@@ -134,6 +134,33 @@ def test_weights_that_leave_nothing_or_too_much():
     assert torch.isfinite(delta[0]) and torch.isnan(delta[1]) and torch.isnan(delta[2])
 
 
+def test_a_weight_that_is_not_finite_spoils_every_row():
+    x = torch.ones(3, 100, device="cuda")
+    x[1, 7] = 0.0
+    for bad in (float("nan"), float("inf")):
+        w = torch.ones(100, device="cuda")
+        w[7] = bad
+        codes, delta, _ = qm.qm_rms_norm_quantize(x, w, 1e-6, "int8")
+        assert torch.isnan(delta).all() and not codes.any()
+
+
+def test_residual_sums_of_any_bf16():
+    """Any finite pair of bf16: the sum is the fp32 sum rounded to nearest even, subnormals, cancellation and overflow among it."""
+    g = torch.Generator().manual_seed(30)
+    bits = torch.randint(0, 1 << 16, (2, 512, 1024), generator=g, dtype=torch.int32)
+    bits[1, 256:] = (bits[0, 256:] ^ 0x8000) + torch.randint(-2048, 2048, (256, 1024), generator=g, dtype=torch.int32)    # neighbours, mostly of the other sign
+    bits &= 0xffff
+    bits = torch.where((bits & 0x7f80) == 0x7f80, bits & 0x807f, bits)
+    x, r = (b.to(torch.int16).view(torch.bfloat16) for b in bits)
+    _, _, z = qm.qm_rms_norm_quantize(x.cuda(), torch.ones(1024, device="cuda"), 1e-6, "int8", residual=r.cuda())
+    with np.errstate(over="ignore"):
+        want = x.float().numpy() + r.float().numpy()
+    finite = np.isfinite(want)
+    got = z.float().cpu().numpy()
+    assert np.array_equal(got[finite].view(np.uint32), layer.round_bf16(want[finite]).view(np.uint32))
+    assert np.array_equal(got[~finite], want[~finite])
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e12, 1e15])
 def test_far_scales(scale):
     x = (torch.randn(4, 512, generator=torch.Generator().manual_seed(10)) * scale).cuda()
