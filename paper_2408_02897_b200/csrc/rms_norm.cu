@@ -420,31 +420,37 @@ qm_status launch_rows(const NormArgs& a, cudaStream_t s) {
   return QM_OK;
 }
 
-template <typename T, int TPR, int N>
-qm_status launch_shape(const NormArgs& a, cudaStream_t s) {
-  return a.res ? launch_rows<T, TPR, N, true>(a, s) : launch_rows<T, TPR, N, false>(a, s);
-}
-
-// The shape for a row of ldc codes.  Two pieces a thread, three where that leaves fewer idle, spread what a row costs as a whole (its
-// reductions, quotients, addresses: as many instructions as a piece) while 100 registers still leave two blocks to an SM.  16384
-// rows, bf16 with a residual, us: 1024 elements (64 threads, 2 pieces) 22.8, (128, 1) 24.8, (64, 4) 27.1; 1025 (64, 3) 37.1, (128, 2)
-// 46.1; 2048 (128, 2) 41.0, (256, 1) 45.3; 4096 (256, 2) 75.3, (128, 4) 80.5, (512, 1) 95.4.  Rows that one SM each can hold are
-// a matter of latency: one piece a thread (1 row of 1024: (128, 1) 1.9, (64, 2) 2.2; of 4096: (512, 1) 2.4, (256, 2) 2.5).
-template <typename T>
+// The shape for a row of ldc codes.  Two pieces a thread or more spread what a row costs as a whole (its reductions, quotients,
+// addresses: as many instructions as a piece) while some 100 registers still leave two blocks to an SM; where the granules of fp32 rows are
+// held beside a residual's, four pieces take 200.  us, (threads to a row, pieces a thread), bf16 with a residual if nothing is said:
+//   16384 x 512 (32, 2) 12.8; 700 (32, 4) 20.1, (64, 2) 24.8; 900 24.9, 27.7; 1024 22.8, 22.8, fp32 with 42.3, 39.5, without 17.6, 20.3;
+//   16384 x 1025 (64, 3) 37.0, (128, 2) 46.0; 2048 (128, 2) 40.8, (64, 4) 43.0; 4096 (256, 2) 75.3, (128, 4) 79.7, (512, 1) 95.4;
+//   8192 x 5000 (256, 4) 55.9, (512, 2) 72.9; fp32 without 46.1, 80.9, with (256, 3) 92.7, (512, 2) 106, (256, 4) 153;
+//   8192 x 8192 (256, 4) 80.7, (512, 2) 80.0; fp32 without 63.4, 95.0, with 199, 144.
+// Rows that one SM each can hold are a matter of latency: one piece a thread (1 row of 1024 (128, 1) 1.9, (64, 2) 2.2; of 4096 (512, 1) 2.4,
+// (256, 2) 2.5), and so, up to 1024, are some thousands (1000 rows of 1024 (64, 2) 3.2, (32, 4) 3.7).
+template <typename T, bool RES>
 qm_status launch_norm(const NormArgs& a, cudaStream_t s) {
+  constexpr bool wide = sizeof(T) == 4 && RES;
   if (a.rows <= sm_count() && a.ldc <= 4096) {
-    if (a.ldc <= 1024) return launch_shape<T, 128, 1>(a, s);
-    return a.ldc <= 2048 ? launch_shape<T, 256, 1>(a, s) : launch_shape<T, 512, 1>(a, s);
+    if (a.ldc <= 1024) return launch_rows<T, 128, 1, RES>(a, s);
+    return a.ldc <= 2048 ? launch_rows<T, 256, 1, RES>(a, s) : launch_rows<T, 512, 1, RES>(a, s);
   }
-  if (a.ldc <= 512) return launch_shape<T, 32, 2>(a, s);
-  if (a.ldc <= 1024) return launch_shape<T, 64, 2>(a, s);
-  if (a.ldc <= 1536) return launch_shape<T, 64, 3>(a, s);
-  if (a.ldc <= 2048) return launch_shape<T, 128, 2>(a, s);
-  if (a.ldc <= 8 * 128 * 3) return launch_shape<T, 128, 3>(a, s);
-  if (a.ldc <= 4096) return launch_shape<T, 256, 2>(a, s);
-  // (fp32 with four pieces takes 198 registers: 8192 elements in 512 threads)
-  if (a.ldc <= 8192) return sizeof(T) == 2 ? launch_shape<__nv_bfloat16, 256, 4>(a, s) : launch_shape<T, 512, 2>(a, s);
-  if (a.ldc <= 16384) return launch_shape<T, 1024, 2>(a, s);
+  if (a.ldc <= 512) return launch_rows<T, 32, 2, RES>(a, s);
+  if constexpr (!wide)
+    if (a.ldc <= 1024 && a.rows >= 32 * sm_count()) return launch_rows<T, 32, 4, RES>(a, s);
+  if (a.ldc <= 1024) return launch_rows<T, 64, 2, RES>(a, s);
+  if (a.ldc <= 1536) return launch_rows<T, 64, 3, RES>(a, s);
+  if (a.ldc <= 2048) return launch_rows<T, 128, 2, RES>(a, s);
+  if (a.ldc <= 8 * 128 * 3) return launch_rows<T, 128, 3, RES>(a, s);
+  if (a.ldc <= 4096) return launch_rows<T, 256, 2, RES>(a, s);
+  if constexpr (wide) {
+    if (a.ldc <= 8 * 256 * 3) return launch_rows<T, 256, 3, RES>(a, s);
+    if (a.ldc <= 8192) return launch_rows<T, 512, 2, RES>(a, s);
+  } else {
+    if (a.ldc <= 8192) return launch_rows<T, 256, 4, RES>(a, s);
+  }
+  if (a.ldc <= 16384) return launch_rows<T, 1024, 2, RES>(a, s);
   QM_CUDA_OK(launch_pdl(rms_norm_long<T>, dim3((unsigned)a.rows), dim3(1024), 0, s, a));
   count_launch();
   return QM_OK;
@@ -461,7 +467,8 @@ qm_status launch_rms_norm(const RowsView& x, const RowsView& residual, void* res
   a.w = weight; a.w_bf16 = weight_dtype == QM_DT_BF16; a.w_vec = reinterpret_cast<uintptr_t>(weight) % 16 == 0;
   a.eps = eps; a.rows = x.rows; a.fmt = fmt;
   a.cols = (int)x.cols; a.ldc = (int)qm_code_ld(x.cols); a.codes = codes; a.delta = delta;
-  return x.dtype == QM_DT_BF16 ? launch_norm<__nv_bfloat16>(a, s) : launch_norm<float>(a, s);
+  if (x.dtype == QM_DT_BF16) return a.res ? launch_norm<__nv_bfloat16, true>(a, s) : launch_norm<__nv_bfloat16, false>(a, s);
+  return a.res ? launch_norm<float, true>(a, s) : launch_norm<float, false>(a, s);
 }
 
 }  // namespace qm

@@ -62,7 +62,7 @@ def test_against_oracle(rows, cols, dtype, fmt):
 
 
 # more rows than SMs (several to a block), a length for each shape of the kernel, rows that start on 16 bytes and rows that do not
-@pytest.mark.parametrize("rows,cols", [(1500, 200), (1700, 513), (900, 1000), (900, 1001), (700, 1530), (701, 2041), (640, 3000), (650, 3001), (600, 4088),
+@pytest.mark.parametrize("rows,cols", [(1500, 200), (1700, 513), (5003, 700), (5000, 1001), (900, 1000), (900, 1001), (700, 1530), (701, 2041), (640, 3000), (650, 3001), (600, 4088),
                                        (610, 4095), (400, 6000), (400, 8185), (300, 12001), (200, 16384)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
