@@ -367,8 +367,8 @@ bool same_or_apart(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int
   return off >= width && pitch - off >= width;
 }
 
-// Extents and pitches whose products stay well inside 64 bits.
-bool sane(int64_t n) { return n < (1ll << 31); }
+// Extents whose tiles' far edges stay inside 32 bits, pitches whose products with them stay well inside 64.
+bool sane(int64_t n) { return n < (1ll << 31) - 1024; }
 bool sane_pitch(int64_t ld) { return ld < (1ll << 30); }
 }  // namespace
 

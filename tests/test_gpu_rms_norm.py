@@ -101,6 +101,25 @@ def test_in_place(cols, which, dtype):
     assert torch.equal(*((r, r0) if which == "x" else (x, x0)))
 
 
+@pytest.mark.parametrize("rows,cols", [(5, 101), (400, 1001), (300, 2048), (700, 4099), (4, 20001)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_columns_beside_one_another(rows, cols, dtype):
+    """x, the residual and its sum as columns of one buffer: the 16 bytes that two of them share are read beside their writing."""
+    buf = torch.cat([make(rows, cols, dtype, 31), make(rows, cols, dtype, 32), make(rows, cols, dtype, 33)], 1)
+    x, z, r = buf[:, :cols], buf[:, cols:2 * cols], buf[:, 2 * cols:]
+    x0, r0 = x.clone(), r.clone()
+    w = torch.ones(cols, device="cuda")
+    check(x0, w, 1e-6, "int8", r0, qm.qm_rms_norm_quantize(x, w, 1e-6, "int8", residual=r, residual_out=z))
+    assert torch.equal(x, x0) and torch.equal(r, r0)
+
+
+def test_all_three_the_same_tensor():
+    x = make(300, 1000, "bf16", 34)
+    x0 = x.clone()
+    w = torch.ones(1000, device="cuda")
+    check(x0, w, 1e-6, "e4m3", x0, qm.qm_rms_norm_quantize(x, w, 1e-6, "e4m3", residual=x, residual_out=x))
+
+
 @pytest.mark.parametrize("cols", [16, 1000, 1024, 4096, 20000])
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_rows_that_are_zero_and_rows_that_are_not_finite(cols, fmt):
@@ -168,7 +187,7 @@ def test_far_scales(scale):
     check(x, w, 1e-6, "int8", None, qm.qm_rms_norm_quantize(x, w, 1e-6, "int8"))
 
 
-@pytest.mark.parametrize("rows,cols", [(70000, 64), (200000, 16), (65537, 40)])
+@pytest.mark.parametrize("rows,cols", [(70000, 64), (200000, 16), (65537, 40), (100003, 1), (3001, 3)])
 def test_many_short_rows(rows, cols):
     x = make(rows, cols, "bf16", 11)
     w = torch.ones(cols, dtype=torch.bfloat16, device="cuda")
