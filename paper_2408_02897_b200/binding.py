@@ -291,8 +291,10 @@ def _vector(t, what, n, dtypes, device):
     return t.data_ptr()
 
 
-# (torch.cuda.current_stream() builds an object, current_device() looks whether CUDA is up: 3 us of a call of 10)
-_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# (torch.cuda.current_stream() builds an object, current_device() looks whether CUDA is up: 3 us of a call of 10; a torch built
+# without CUDA has the public functions only, which raise when they are called)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _on(stream):
