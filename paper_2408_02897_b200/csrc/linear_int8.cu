@@ -64,7 +64,7 @@ __device__ __forceinline__ float activate(float g) {
     q = fmaf(q, t, 1.5611439f); q = fmaf(q, t, -2.708909f); q = fmaf(q, t, 2.1119456f); q = fmaf(q, t, -1.0494819f);
     q = fmaf(q, t, 0.6094263f); q = fmaf(q, t, 0.5445073f); q = fmaf(q, t, 1.4499226f); q = fmaf(q, t, -2.1845343f);
     const float half = 0.5f * g, tail = half * (t * ex2_approx(fmaf(g * g, -0.72134752f, q)));
-    return g < 0.f ? tail : g - tail;
+    return g < 0.f ? tail : g - fmaxf(tail, 0.f);             // (of an infinite gate the tail is Inf times 0; fmaxf makes 0 of a NaN)
   }
   const float t = ACT == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
   return g * 9.5367432e-7f * rcp_approx(fmaf(ex2_approx(-1.442695f * t), 9.5367432e-7f, 9.5367432e-7f));
