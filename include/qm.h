@@ -326,8 +326,8 @@ qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delt
 /*
  * qm_gated_linear_int8: h = act(g) * u with g = x . gate^T and u = x . up^T as in qm_linear_int8 (no bias), both
  * products, the activation (qm_act) and the multiplication in one kernel; g and u are not written.  codes_gate and codes_up may be
- * two halves of one tensor.  act(g) is evaluated in fp32; where g is so negative that act(g) is below fp32's
- * range, h is 0 (of either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times
+ * two halves of one tensor.  act(g) is evaluated in fp32; what is below fp32's normal numbers may come out as 0 (of
+ * either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times
  * Inf).  Other arguments as for qm_linear_int8.
  */
 qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_gate,

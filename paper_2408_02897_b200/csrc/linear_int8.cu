@@ -54,8 +54,9 @@ constexpr int kNoAct = -1;
 //    exp(z^2) / t) interpolated at Chebyshev points for z up to 10, degree 8: 6.3e-8 off, which with fp32's roundings is 4.2 half steps of |g|
 //    (erff and 1 + erf are as many, in three times the instructions).  To the base 2, with |g| for z.
 //  The others: g / (1 + exp(-t)), t = g or twice the tanh's argument: 1/2 (1 + tanh) is that quotient, and unlike 1 + tanh it keeps
-//    its relative precision where g is negative.  Both sides of the quotient are scaled by 2^-20, because the approximate
-//    reciprocal gives 0 from 2^126 on; beyond exp's range the quotient is 0.
+//    its relative precision where g is negative.  1 / (1 + exp(-t)) is s / (s exp(-t) + s) with s = 2^-20, so that the exponential stays
+//    inside fp32 and the approximate reciprocal, which gives 0 from 2^126 on, above 0 until g times the quotient is far below
+//    fp32's normal numbers (t = -101).  g comes last: scaled by s a small gate would lose its bits.
 template <int ACT>
 __device__ __forceinline__ float activate(float g) {
   if (ACT == QM_ACT_GELU) {
@@ -67,7 +68,8 @@ __device__ __forceinline__ float activate(float g) {
     return g < 0.f ? tail : g - fmaxf(tail, 0.f);             // (of an infinite gate the tail is Inf times 0; fmaxf makes 0 of a NaN)
   }
   const float t = ACT == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
-  return g * 9.5367432e-7f * rcp_approx(fmaf(ex2_approx(-1.442695f * t), 9.5367432e-7f, 9.5367432e-7f));
+  constexpr float kS = 9.5367432e-7f;
+  return g * (kS * rcp_approx(ex2_approx(fmaf(-1.442695f, t, -20.f)) + kS));
 }
 
 __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {

@@ -43,3 +43,45 @@ def test_infinite_gates(act, M, K, dt):
     assert h[0] == inf and np.isnan(h[1]) and np.isnan(h[2])
     assert abs(h[3] / 1.5e38 - 1) <= 2.0 ** -8
     assert np.array_equal(h[4:], clean[4:])
+
+
+def reference(g, act):
+    """act(g), t of its quotient g / (1 + exp(-t)) and Phi(-|g|), in 64 bits."""
+    t = g if act == "silu" else 2 * np.sqrt(2 / np.pi) * (g + 0.044715 * g ** 3)
+    phi = 0.5 * np.array([layer.math.erfc(abs(v) / 2 ** 0.5) for v in g])
+    return layer.activation(g, act), np.abs(t), phi
+
+
+def allowed(g, act):
+    """act(g) and what its evaluation in fp32 may be off by."""
+    a, t, phi = reference(g, act)
+    if act == "gelu":
+        return a, U * (np.abs(g) * phi * (1.2 * g * g + 22) + np.abs(a)) + 2.0 ** -125
+    # the exponent's roundings (its constant's among them), |t| times those of the tanh's argument; exp, the sum, the reciprocal, g
+    off = (1.3 if act == "silu" else 7.3) * t + 24
+    return a, U * off * np.abs(a) + 2.0 ** -139
+
+
+def check(gates, act, dt, M=3, K=16):
+    gates = gates.float()
+    h = gated(gates, torch.ones(len(gates)), act, dt, M, K)
+    a, off = allowed(gates.double().numpy(), act)
+    if dt is torch.bfloat16:                                         # rounded once more: half a step, a subnormal one at least
+        off = off + np.maximum(2.0 ** -8 * (np.abs(a) + off), 2.0 ** -134)
+    bad = np.abs(h - a) > off
+    assert not bad.any(), (gates[bad][:5], h[bad][:5], a[bad][:5], (np.abs(h - a) / off)[bad].max())
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act,lo,hi", [("silu", -105, -80), ("gelu_tanh", -11.5, -9), ("gelu", -14.5, -12)])
+def test_gates_whose_activation_nears_the_end_of_fp32(act, lo, hi, dt):
+    """As long as act(g) is a normal number of fp32 it is there, although exp(-g) is not."""
+    check(torch.linspace(lo, hi, 8000, dtype=torch.float64), act, dt)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ACTS)
+def test_tiny_and_huge_gates(act, dt):
+    """act(g) is g / 2 next to zero and g, or nothing, far from it, with all of fp32's bits."""
+    size = 10.0 ** torch.linspace(-37.9, 38.4, 4000, dtype=torch.float64)
+    check(torch.cat([size, -size]), act, dt)
