@@ -326,8 +326,10 @@ qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delt
 /*
  * qm_gated_linear_int8: h = act(g) * u with g = x . gate^T and u = x . up^T as in qm_linear_int8 (no bias), both
  * products, the activation (qm_act) and the multiplication in one kernel; g and u are not written.  codes_gate and codes_up may be
- * two halves of one tensor.  act(g) is evaluated in fp32; what is below fp32's normal numbers may come out as 0 (of
- * either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times
+ * two halves of one tensor.  act(g) is evaluated in fp32 by approximate exponentials and reciprocals.  In units of 2^-24 it is off by at
+ * most 12 |act(g)| (SiLU), (6 |t| + 12) |act(g)| (GELU_TANH, t = 2 sqrt(2/pi) (g + 0.044715 g^3)) and |act(g)| + (1.2 g^2 + 22) |g| Phi(-|g|)
+ * (GELU, Phi the normal law's integral), where the output is bf16 (1.3 |g| + 24) |act(g)| and (7.3 |t| + 24) |act(g)| for the
+ * first two; what is below fp32's normal numbers may come out as 0 (of either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times
  * Inf).  Other arguments as for qm_linear_int8.
  */
 qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_gate,

@@ -46,18 +46,23 @@ __device__ __forceinline__ float rcp_approx(float x) {
 }
 
 // One product.  The gated kernels are compiled for each activation: chosen in the epilogue's loop it is a branch for every output, under which no
-// other output's exponential runs (8192 x 4096 x 1024 54 us, now 50); chosen ahead of the loop, its three copies do not stay in the
+// other output's exponential runs (8192 x 4096 x 1024 54 us instead of 50); chosen ahead of the loop, its three copies do not stay in the
 // instruction cache (63 us).
 constexpr int kNoAct = -1;
+
 // act(g) in fp32.
 //  GELU: g Phi(g), Phi(-|g|) = erfc(z) / 2 with z = |g| / sqrt 2 and erfc(z) = t exp(-z^2 + Q(t)), t = 1 / (1 + 0.39 z).  Q is log(erfc(z)
-//    exp(z^2) / t) interpolated at Chebyshev points for z up to 10, degree 8: 6.3e-8 off, which with fp32's roundings is 4.2 half steps of |g|
-//    (erff and 1 + erf are as many, in three times the instructions).  To the base 2, with |g| for z.
+//    exp(z^2) / t) interpolated at Chebyshev points for z up to 10, degree 8.  To the base 2, with |g| for z.  What is off of |g| Phi(-|g|) is
+//    at most 1.2 g^2 + 22 half steps of it (the exponent's roundings grow with g^2; the polynomial's, the fit's, ex2's 4 and the reciprocal's
+//    are the 22), next to zero 11 half steps of |g| (4.2 seen).  1/2 g (1 + erff) has 3 there, in more instructions, and loses the
+//    negative tail, which this keeps.
 //  The others: g / (1 + exp(-t)), t = g or twice the tanh's argument: 1/2 (1 + tanh) is that quotient, and unlike 1 + tanh it keeps
 //    its relative precision where g is negative.  1 / (1 + exp(-t)) is s / (s exp(-t) + s) with s = 2^-20, so that the exponential stays
 //    inside fp32 and the approximate reciprocal, which gives 0 from 2^126 on, above 0 until g times the quotient is far below
 //    fp32's normal numbers (t = -101).  g comes last: scaled by s a small gate would lose its bits.
-template <int ACT>
+//    The exponent's rounding and its constant's are |t| half steps of exp or, next to zero, 20: less than a bf16 output shows.  For fp32 outputs
+//    the exponent's whole part is taken out exactly: 12 half steps at any g, for 8192 x 4096 x 1024 63 us instead of 59.
+template <typename T, int ACT>
 __device__ __forceinline__ float activate(float g) {
   if (ACT == QM_ACT_GELU) {
     const float t = rcp_approx(fmaf(0.27577165f, fabsf(g), 1.f));
@@ -69,7 +74,16 @@ __device__ __forceinline__ float activate(float g) {
   }
   const float t = ACT == QM_ACT_SILU ? g : 1.5957691f * fmaf(0.044715f * g * g, g, g);
   constexpr float kS = 9.5367432e-7f;
-  return g * (kS * rcp_approx(ex2_approx(fmaf(-1.442695f, t, -20.f)) + kS));
+  float e;
+  if (sizeof(T) == 4) {
+    // s exp(-t) = 2^(n - 20) 2^r; beyond the limits it is nothing next to s, or the quotient nothing
+    const float u = fmaxf(fminf(t, 73.f), -102.f), z = fmaf(-1.442695f, u, 12582912.f), n = z - 12582912.f;
+    const float r = fmaf(-1.925963e-8f, u, fmaf(-1.442695f, u, -n));
+    e = ex2_approx(r) * __uint_as_float((__float_as_uint(z) << 23) + (107u << 23));
+  } else {
+    e = ex2_approx(fmaf(-1.442695f, t, -20.f));
+  }
+  return g * (kS * rcp_approx(e + kS));
 }
 
 __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
@@ -289,7 +303,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
         if (GATED)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) y[i] = activate<ACT>(y[i]) * up[i];
+          for (int i = 0; i < 16; ++i) y[i] = activate<T, ACT>(y[i]) * up[i];
         T* p = out + (int64_t)(m0 + c) * a.ld + n;
 #pragma unroll
         for (int i = 0; i < 16; ++i, p += a.ld)
@@ -352,7 +366,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         }
         if (GATED)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) y[k] = activate<ACT>(y[k]) * up[k];
+          for (int k = 0; k < 4; ++k) y[k] = activate<T, ACT>(y[k]) * up[k];
 #pragma unroll
         for (int k = 0; k < 4; ++k) if (!ok) y[k] = nan_f();
         store4(out + (int64_t)(m0 + row) * a.ld + n0 + j, y, cols, a.vec);
@@ -372,7 +386,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 // Bound by the tensor cores from contractions of 2048 on (8192 x 8192 x 4096 167 us, 3.3 POP/s; 531 cycles for 128 entries, 512 at the
 // pipe's peak), below that by the output: 16384 x 4096 x 1024 takes 54 us, 44 without its stores, and 35 with a contraction
 // of 128, which is what a fill of those 134 MB takes (34.8).  Bulk stores of the staged rows and plain ones measured the same; four stages
-// 59, cache hints on the stores 53 to 54.  The gated form's epilogue alone (contraction of 128) is 39 us for 8192 x 4096 outputs, half
+// 59, cache hints on the stores 53 to 54.  The gated form's epilogue alone (contraction of 128) is 37 us for 8192 x 4096 outputs, half
 // of it the activation, under 44 of MMAs.
 struct ManyArgs {
   int64_t M, N;
@@ -621,7 +635,7 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             }
             if (GATED)
 #pragma unroll
-              for (int k = 0; k < 16; ++k) y[k] = activate<ACT>(y[k]) * up[k];
+              for (int k = 0; k < 16; ++k) y[k] = activate<T, ACT>(y[k]) * up[k];
 #pragma unroll
             for (int k = 0; k < 16; ++k) if (!ok) y[k] = nan_f();
             stage_16x32(smem_u32(stage), lane, 16 * hf, part, y, T());

@@ -52,20 +52,22 @@ def reference(g, act):
     return layer.activation(g, act), np.abs(t), phi
 
 
-def allowed(g, act):
-    """act(g) and what its evaluation in fp32 may be off by."""
+def stated(g, act, dt):
+    """What include/qm.h allows act(g) to be off by, in fp32."""
     a, t, phi = reference(g, act)
     if act == "gelu":
         return a, U * (np.abs(g) * phi * (1.2 * g * g + 22) + np.abs(a)) + 2.0 ** -125
-    # the exponent's roundings (its constant's among them), |t| times those of the tanh's argument; exp, the sum, the reciprocal, g
-    off = (1.3 if act == "silu" else 7.3) * t + 24
+    if dt is torch.float32:
+        off = 12 if act == "silu" else 6 * t + 12
+    else:
+        off = (1.3 if act == "silu" else 7.3) * t + 24
     return a, U * off * np.abs(a) + 2.0 ** -139
 
 
 def check(gates, act, dt, M=3, K=16):
     gates = gates.float()
     h = gated(gates, torch.ones(len(gates)), act, dt, M, K)
-    a, off = allowed(gates.double().numpy(), act)
+    a, off = stated(gates.double().numpy(), act, dt)
     if dt is torch.bfloat16:                                         # rounded once more: half a step, a subnormal one at least
         off = off + np.maximum(2.0 ** -8 * (np.abs(a) + off), 2.0 ** -134)
     bad = np.abs(h - a) > off
@@ -85,3 +87,14 @@ def test_tiny_and_huge_gates(act, dt):
     """act(g) is g / 2 next to zero and g, or nothing, far from it, with all of fp32's bits."""
     size = 10.0 ** torch.linspace(-37.9, 38.4, 4000, dtype=torch.float64)
     check(torch.cat([size, -size]), act, dt)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M,K", KERNELS)
+def test_ordinary_gates_stay_within_the_stated_bounds(act, M, K, dt):
+    """Densely from -16 to 16, and for the quotients as far as they are normal numbers."""
+    gates = torch.linspace(-16, 16, 12001, dtype=torch.float64)
+    if act == "silu":
+        gates = torch.cat([gates, torch.linspace(-88, 88, 12000, dtype=torch.float64)])
+    check(gates, act, dt, M, K)
