@@ -292,7 +292,7 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
  *   v = z * weight in fp32;  d = max|v| / qmax;  codes = sat(RTNE(v / d)), as qm_quantize(v) gives them
  *   delta = d / sqrt(mean(z^2) + eps)
  * so that code * delta stands for z * weight / rms(z): the norm's factor is one positive number for the
- * row and cancels in Eq. 1's quotient, so the codes do not depend on how the squares were summed (fp32).
+ * row and cancels in Eq. 1's quotient, so the codes do not depend on how the squares were summed (fp32, compensated beyond 16384 columns).
  *  x, residual, residual_out   bf16 or fp32 (`dtype`), rows ld_* elements apart.  residual and residual_out are
  *             both NULL (z = x) or both given; residual_out receives z and may be x or residual itself
  *             (same pointer, same pitch), no other overlap.

@@ -359,8 +359,9 @@ __global__ void __launch_bounds__(block_threads(TPR)) rms_norm_rows(const NormAr
   }
 }
 
-// Rows that no block holds in registers: a block per row, v formed again for the codes from x and residual, or where
-// residual_out is one of them, from z as this thread has left it.
+// Rows that no block holds in registers: a block per row, v formed again for the codes from x or, with a residual, from z as this
+// thread has left it.  A thread's squares may be a million, so its sum carries along what each addition has rounded off (Kahan): without that
+// 2^24 equal elements were 5e-5 off, and a sum in 64 bits takes 433 us for 2048 x 32768 where this takes 289 and the plain one 278 (bf16 with a residual).
 template <typename T>
 __global__ void __launch_bounds__(1024) rms_norm_long(const NormArgs a) {
   pdl_prologue();
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(1024) rms_norm_long(const NormArgs a) {
   const T* const r = static_cast<const T*>(a.res) + row * a.ld_res;
   T* const z = static_cast<T*>(a.res_out) + row * a.ld_out;
   auto weight = [&](int c) { return a.w_bf16 ? Loader<__nv_bfloat16>::load1(a.w, c) : Loader<float>::load1(a.w, c); };
-  float sum = 0.f, top = 0.f;
+  float sum = 0.f, over = 0.f, top = 0.f;
   for (int c = threadIdx.x; c < a.cols; c += 1024) {
     float zf = (float)x[c];
     if (a.res) {
@@ -377,7 +378,9 @@ __global__ void __launch_bounds__(1024) rms_norm_long(const NormArgs a) {
       z[c] = rounded;
       zf = (float)rounded;
     }
-    sum = fmaf(zf, zf, sum);
+    const float term = fmaf(zf, zf, -over), next = sum + term;
+    over = (next - sum) - term;
+    sum = next;
     top = max_abs(top, zf * weight(c));
   }
   __shared__ float sums[32];
