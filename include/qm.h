@@ -299,7 +299,7 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
  *  weight     `cols` values, bf16 or fp32 (`weight_dtype`).
  *  eps        positive and normal in fp32.
  *  codes      [rows][qm_code_ld(cols)], 16-byte aligned, padding zero;  delta [rows] fp32.
- * A row whose v is all zero gets delta = 1.  A row with a NaN or Inf in z or v (0 times an Inf among the weights is one), or whose sum
+ * A row whose v is all zero gets delta = 1, and so does, with codes 0, one so small that d is 0 in fp32.  A row with a NaN or Inf in z or v (0 times an Inf among the weights is one), or whose sum
  * of squares leaves fp32, gets delta = NaN and codes 0; other rows are as they would be without it.
  */
 qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int32_t dtype,

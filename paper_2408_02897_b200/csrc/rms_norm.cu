@@ -220,10 +220,11 @@ __device__ __noinline__ uint32_t code_far(float v, float own, int fmt) {
 
 __host__ __device__ constexpr int block_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
 
-// What the threads of a row agree on: Eq. 1's scale of its v, and the row's delta (in the thread that stores it).
+// What the threads of a row agree on: Eq. 1's scale of its v, and the row's delta (in the thread that stores it).  A scale that is 0 in
+// fp32, though v is not, has no quotients: such a row counts as one of zeros.
 __device__ __forceinline__ float row_delta(const NormArgs& a, float own, uint32_t top_bits, float sum, bool finite) {
   if (!finite) return __int_as_float(0x7fffffff);
-  return top_bits == 0 ? 1.f : own * (1.f / sqrtf(sum / (float)a.cols + a.eps));
+  return top_bits == 0 || own == 0.f ? 1.f : own * (1.f / sqrtf(sum / (float)a.cols + a.eps));
 }
 
 // Shared memory: a ring of rows on their way in.  A warp's piece is 256 elements: 32 x kQ granules and one more, for rows that do not
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) rms_norm_rows(const NormAr
         for (int j = 0; j < 4; ++j) {
           float lo, hi;
           halves(v[i][j], lo, hi);
-          if (finite) q[j >> 1] |= (code_far(lo, own, a.fmt) | code_far(hi, own, a.fmt) << 8) << (16 * (j & 1));
+          if (finite && own != 0.f) q[j >> 1] |= (code_far(lo, own, a.fmt) | code_far(hi, own, a.fmt) << 8) << (16 * (j & 1));
         }
         *reinterpret_cast<uint2*>(codes + c) = make_uint2(q[0], q[1]);
       }
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(1024) rms_norm_long(const NormArgs a) {
   const T* const from = a.res ? z : x;
   uint8_t* const codes = a.codes + row * a.ldc;
   for (int c = threadIdx.x; c < a.ldc; c += 1024)
-    codes[c] = finite && c < a.cols ? (uint8_t)code_far((float)from[c] * weight(c), own, a.fmt) : (uint8_t)0;
+    codes[c] = finite && own != 0.f && c < a.cols ? (uint8_t)code_far((float)from[c] * weight(c), own, a.fmt) : (uint8_t)0;
 }
 
 template <typename T, int TPR, int N, bool RES>

@@ -51,3 +51,19 @@ def test_scales_by_the_depth_of_their_sums(rows, cols, dtype, residual):
     want = expected((z if residual else x).float().cpu().numpy(), w.float().cpu().numpy(), float(np.float32(1e-6)), 127)
     off = np.abs(delta.double().cpu().numpy() / want - 1)
     assert (off <= (REGISTERS if cols <= 16384 else LONG)).all(), off.max() / U
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3", "e5m2"])
+@pytest.mark.parametrize("cols", [40, 1000, 1024, 4096, 20001])
+def test_rows_whose_scale_is_below_fp32(cols, fmt):
+    """max|v| / qmax is 0 in fp32 although max|v| is not: the row counts as one of zeros, and its neighbours do not see it."""
+    x = torch.randn(4, cols, generator=torch.Generator().manual_seed(1))
+    x[1] = 0.0
+    x[1, ::3] = 2.0 ** -149
+    x[2, :] = -2.0 ** -148
+    w = torch.ones(cols)
+    codes, delta, _ = qm.qm_rms_norm_quantize(x.cuda(), w.cuda(), 1e-6, fmt)
+    assert not codes[0, 1:3].any() and not codes[0, :, cols:].any()
+    assert (delta[1:3] == 1.0).all()
+    _, want, _ = layer.rms_norm_quantize(x[[0, 3]].numpy(), w.numpy(), 1e-6, fmt)
+    assert np.array_equal(codes[0, [0, 3], :cols].cpu().numpy(), want)
