@@ -224,7 +224,10 @@ __host__ __device__ constexpr int block_threads(int tpr) { return tpr < 256 ? 25
 // fp32, though v is not, has no quotients: such a row counts as one of zeros.
 __device__ __forceinline__ float row_delta(const NormArgs& a, float own, uint32_t top_bits, float sum, bool finite) {
   if (!finite) return __int_as_float(0x7fffffff);
-  return top_bits == 0 || own == 0.f ? 1.f : own * (1.f / sqrtf(sum / (float)a.cols + a.eps));
+  if (top_bits == 0 || own == 0.f) return 1.f;
+  const float mean = sum / (float)a.cols, square = mean + a.eps;
+  // (a quarter of either where their sum leaves fp32, which its root does not)
+  return own * (square < INFINITY ? 1.f / sqrtf(square) : 0.5f / sqrtf(0.25f * mean + 0.25f * a.eps));
 }
 
 // Shared memory: a ring of rows on their way in.  A warp's piece is 256 elements: 32 x kQ granules and one more, for rows that do not

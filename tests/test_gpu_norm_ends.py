@@ -67,3 +67,17 @@ def test_rows_whose_scale_is_below_fp32(cols, fmt):
     assert (delta[1:3] == 1.0).all()
     _, want, _ = layer.rms_norm_quantize(x[[0, 3]].numpy(), w.numpy(), 1e-6, fmt)
     assert np.array_equal(codes[0, [0, 3], :cols].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("cols", [1, 8, 300, 20000])
+@pytest.mark.parametrize("eps", [1.2e-38, 1e-20, 1e20, 3.4e38])
+def test_scales_under_any_eps(cols, eps):
+    """mean(z^2) + eps may leave fp32 where its root does not."""
+    eps = float(np.float32(eps))
+    x = torch.full((3, cols), 1.0)
+    x[0] = 1.8e19 / cols ** 0.5 * 0.99                               # the sum of squares is near fp32's largest
+    x[2] = 3e-3
+    codes, delta, _ = qm.qm_rms_norm_quantize(x.cuda(), torch.ones(cols, device="cuda"), eps, "int8")
+    want = expected(x.numpy(), np.ones(cols, np.float32), eps, 127)
+    off = np.abs(delta.double().cpu().numpy() / want - 1)
+    assert (off <= REGISTERS).all() and (codes[0, :, :cols] == 127).all()
