@@ -108,6 +108,11 @@ __device__ __forceinline__ void activate(float& g0, float& g1) {
   halves(mul2(g, mul2(both(kS), pair_of(rcp_approx(x0), rcp_approx(x1)))), g0, g1);
 }
 
+// An output of its sum, the same roundings in every epilogue (said here, so that the compiler makes the same instructions of it everywhere;
+// with the sum as the first factor it gives one of the kernels 72 registers instead of 80, and 512 x 4096 x 1024 takes 6.5 us instead of 5.6).
+__device__ __forceinline__ float output_of(uint32_t sum, float dx, float dw, float bias) { return fmaf(dx * dw, (float)(int)sum, bias); }
+__device__ __forceinline__ float output_of(uint32_t sum, float dx, float dw) { return dx * dw * (float)(int)sum; }
+
 __device__ __forceinline__ float load_bias(const Scales& s, int64_t n) {
   if (!s.bias) return 0.f;
   return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
@@ -319,9 +324,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float dxv = sh->dx[c + i];                                    // (rows beyond the last: not stored)
-          y[i] = (float)(int)r[i] * (dxv * dw[0]);
-          if (GATED) up[i] = (float)(int)u[i] * (dxv * du[0]);
-          else y[i] += bias[0];
+          y[i] = GATED ? output_of(r[i], dxv, dw[0]) : output_of(r[i], dxv, dw[0], bias[0]);
+          if (GATED) up[i] = output_of(u[i], dxv, du[0]);
         }
         if (GATED)
 #pragma unroll
@@ -385,9 +389,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
         float y[4], up[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          y[k] = (float)gs[k] * (dxv * dw[k]);
-          if (GATED) up[k] = (float)us[k] * (dxv * du[k]);
-          else y[k] += bias[k];
+          y[k] = GATED ? output_of(gs[k], dxv, dw[k]) : output_of(gs[k], dxv, dw[k], bias[k]);
+          if (GATED) up[k] = output_of(us[k], dxv, du[k]);
         }
         if (GATED)
 #pragma unroll
@@ -656,10 +659,9 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               const int i = k >> 2;
-              const float dxv = dx[2 * hf + ((k >> 1) & 1)];
-              y[k] = (float)(int)r[hf][k] * (dxv * (k & 1 ? d[i].y : d[i].x));
-              if (GATED) up[k] = (float)(int)u[hf][k] * (dxv * (k & 1 ? e[i].y : e[i].x));
-              else y[k] += k & 1 ? b[i].y : b[i].x;
+              const float dxv = dx[2 * hf + ((k >> 1) & 1)], dwv = k & 1 ? d[i].y : d[i].x;
+              y[k] = GATED ? output_of(r[hf][k], dxv, dwv) : output_of(r[hf][k], dxv, dwv, k & 1 ? b[i].y : b[i].x);
+              if (GATED) up[k] = output_of(u[hf][k], dxv, k & 1 ? e[i].y : e[i].x);
             }
             if (GATED)
 #pragma unroll
