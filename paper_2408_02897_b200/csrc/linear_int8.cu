@@ -278,8 +278,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     // the columns back when the epilogue has read them (or given up), ahead of the wait for the peers' sums
     if (a.split > 1) { cluster_wait(); cluster_arrive(); }
     wait_limited(smem_u32(&sh->read), 0, a.waits.limit_ns);
-    if (sh->abort_flag) {                          // give-up path: MMAs that nobody has waited for
-      __syncwarp();
+    // give-up path: MMAs that nobody has waited for.  The loading warp may flag the CTA at this moment: one decision for the warp
+    if (__any_sync(0xffffffffu, *w.abort_flag)) {
       if (lead) tc_commit_one(smem_u32(&sh->drain));
       wait_limited(smem_u32(&sh->drain), 0, a.waits.limit_ns);
     }

@@ -100,3 +100,37 @@ assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
     for threads in (False, True):
         r = subprocess.run([sys.executable, "-c", code.format(threads=threads)], capture_output=True, text=True, timeout=300)
         assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.fixture
+def starved_producer():
+    L = qm.lib()
+    L.qm_debug_set_wait_limit_ns(2_000_000)                            # 2 ms instead of 1 s
+    yield L
+    L.qm_debug_stop_producer_after(0xffffffff)
+    L.qm_debug_set_wait_limit_ns(0)
+
+
+# (on 148 SMs) one row, and 40, split eight ways over a cluster; 200 rows, one CTA a tile
+@pytest.mark.parametrize("M,N,K", [(1, 1000, 8192), (40, 256, 8192), (200, 6000, 384)])
+@pytest.mark.parametrize("stop_after", [0, 1, 2])
+@pytest.mark.parametrize("gated", [False, True])
+def test_a_kernel_that_gave_up_frees_its_tensor_memory(starved_producer, M, N, K, stop_after, gated):
+    """Many calls that give up one after the other, on two streams: each returns, and a full one behind them is right."""
+    _, x = codes(M, K, 7)
+    _, w = codes(N, K, 8)
+    dx, dw = torch.full((M,), 0.01, device="cuda"), torch.full((N,), 0.0001, device="cuda")
+
+    def call(stream=None):
+        return qm.qm_gated_linear_int8(x, dx, w, dw, w, dw, K, stream=stream) if gated else qm.qm_linear_int8(x, dx, w, dw, K, stream=stream)
+    want = call()
+    torch.cuda.synchronize()
+    starved_producer.qm_debug_stop_producer_after(stop_after)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [call(streams[i % 2]) for i in range(8)]
+    torch.cuda.synchronize()
+    for y in got:
+        bad = y.isnan()
+        assert torch.equal(y[~bad], want[~bad]) and (stop_after or bad.all())
+    starved_producer.qm_debug_stop_producer_after(0xffffffff)
+    assert torch.equal(call(), want)
