@@ -432,7 +432,7 @@ constexpr uint32_t kManyStageBytes = 2 * kBlockBytes;
 constexpr uint32_t kOutBytes = 32 * 128;       // of output on its way per epilogue warp: 32 rows of 128 bytes
 struct SharedMany {
   uint64_t full[kManyStages], empty[kManyStages], tmem_full[2], tmem_empty[2], drain;
-  uint32_t tmem_base, abort_flag, issued, pad;
+  uint32_t tmem_base, abort_flag, issued, peer_gave_up, peer_issued, pad[3];
   alignas(16) float dw[2][256], bias[2][256];
 };
 
@@ -523,7 +523,7 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       mbar_init(smem_u32(&sh->tmem_empty[b]), 2 * kEpiWarps);
     }
     mbar_init(smem_u32(&sh->drain), 1);
-    sh->abort_flag = 0; sh->issued = 0;
+    sh->abort_flag = 0; sh->issued = 0; sh->peer_gave_up = 0; sh->peer_issued = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -702,11 +702,19 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 
   tc_fence_before();
   __syncthreads();
-  if (sh->abort_flag) {
-    // give-up path: loads (both CTAs' complete on the leader's barriers) and MMAs that nobody has waited for
+  // Neither CTA loads from here on.  They go through the give-up path together, if either has given up.
+  if (threadIdx.x == 0) {
+    if (rank == 1) sts_cluster(map_to_cta(smem_u32(&sh->peer_issued), 0), sh->issued);
+    if (sh->abort_flag) sts_cluster(map_to_cta(smem_u32(&sh->peer_gave_up), rank ^ 1u), 1u);
+  }
+  cluster_sync();
+  if (sh->abort_flag | sh->peer_gave_up) {
+    // loads (both CTAs' complete on the leader's barriers) and MMAs that nobody has waited for.  A commit that came as the leader gave up may
+    // have let the peer load further: bytes that the leader has yet to expect
     if (threadIdx.x == 0 && rank == 0) {
-      const uint32_t n = sh->issued;
-      for (uint32_t g = n > (uint32_t)kManyStages ? n - kManyStages : 0u; g < n; ++g)
+      const uint32_t n = sh->issued, most = max(n, sh->peer_issued);
+      for (uint32_t g = n; g < most; ++g) mbar_expect_tx(smem_u32(&sh->full[g % kManyStages]), kManyStageBytes);
+      for (uint32_t g = most > (uint32_t)kManyStages ? most - kManyStages : 0u; g < most; ++g)
         wait_limited(smem_u32(&sh->full[g % kManyStages]), (g / kManyStages) & 1, a.waits.limit_ns);
     }
     if (warp == 1 && rank == 0) {
@@ -714,9 +722,8 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sh->drain)) : "memory");
       wait_limited(smem_u32(&sh->drain), 0, a.waits.limit_ns);
     }
-    __syncthreads();
+    cluster_sync();
   }
-  cluster_sync();
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();

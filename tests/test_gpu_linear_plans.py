@@ -111,8 +111,9 @@ def starved_producer():
     L.qm_debug_set_wait_limit_ns(0)
 
 
-# (on 148 SMs) one row, and 40, split eight ways over a cluster; 200 rows, one CTA a tile
-@pytest.mark.parametrize("M,N,K", [(1, 1000, 8192), (40, 256, 8192), (200, 6000, 384)])
+# (on 148 SMs) one row, and 40, split eight ways over a cluster; 200 rows, one CTA a tile; CTA pairs with a tile each, plain and gated; pairs
+# with two tiles, gated three
+@pytest.mark.parametrize("M,N,K", [(1, 1000, 8192), (40, 256, 8192), (200, 6000, 384), (257, 7680, 128), (400, 2816, 1024), (600, 9000, 512)])
 @pytest.mark.parametrize("stop_after", [0, 1, 2])
 @pytest.mark.parametrize("gated", [False, True])
 def test_a_kernel_that_gave_up_frees_its_tensor_memory(starved_producer, M, N, K, stop_after, gated):
