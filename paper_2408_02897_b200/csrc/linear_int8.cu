@@ -15,6 +15,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "qm_internal.h"
 #include "tc_ptx.cuh"
@@ -754,13 +755,13 @@ bool out_map(CUtensorMap* m, void* base, int dtype, int64_t M, int64_t N, int64_
 }
 
 template <typename K, typename... P>
-qm_status launch_cluster(K kern, bool (&ready)[kMaxDevices], size_t smem, size_t smem_most, unsigned grid, unsigned cluster,
+qm_status launch_cluster(K kern, std::atomic<bool> (&ready)[kMaxDevices], size_t smem, size_t smem_most, unsigned grid, unsigned cluster,
                          cudaStream_t s, const P&... params) {
   const int dev = current_device();
   if (dev < 0) return QM_ERR_UNSUPPORTED;
-  if (!ready[dev]) {
+  if (!ready[dev].load(std::memory_order_acquire)) {
     QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_most));
-    ready[dev] = true;
+    ready[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
@@ -820,7 +821,7 @@ constexpr size_t kFewSmem = 1024 + kFewRing + sizeof(SharedFew);
 template <typename T, int ACT>
 qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   constexpr bool GATED = ACT != kNoAct;
-  static bool ready[kMaxDevices] = {};
+  static std::atomic<bool> ready[kMaxDevices];
   FewArgs a{};
   a.M = l.M; a.N = l.N;
   a.num_kb = (int)((l.K + kBlock - 1) / kBlock);
@@ -856,7 +857,7 @@ qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
 template <typename T, int ACT>
 qm_status launch_many(const LinearArgs& l, cudaStream_t s) {
   constexpr bool GATED = ACT != kNoAct;
-  static bool ready[kMaxDevices] = {};
+  static std::atomic<bool> ready[kMaxDevices];
   // all of an SM's shared memory: a CTA that holds tensor memory waits for its peer here, so neither may have to wait for another kernel's
   constexpr size_t smem = 232448;
   static_assert(1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + sizeof(SharedMany) <= smem, "shared memory of a CTA");

@@ -4,6 +4,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "qm_internal.h"
 
 namespace qm {
@@ -288,13 +290,16 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapFloatOOBfill);
 
 inline EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
+  static std::atomic<EncodeTiledFn> found{nullptr};
+  EncodeTiledFn fn = found.load(std::memory_order_relaxed);
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
+        qres == cudaDriverEntryPointSuccess) {
       fn = reinterpret_cast<EncodeTiledFn>(p);
+      found.store(fn, std::memory_order_relaxed);
+    }
   }
   return fn;
 }
