@@ -261,7 +261,7 @@ qm_status qm_quantize_formats(const qm_operand* x, int32_t n_fmt, const int32_t*
  * accumulator [batch][M][N]: int32 for INT8 x INT8, fp32 bit patterns for FP8.
  * Mixing INT8 with an FP8 format is QM_ERR_UNSUPPORTED.  use_simt != 0 selects
  * the CUDA-core kernel (any K; test cross-check); the tensor-core kernel needs
- * K to be a multiple of 16.
+ * K to be a multiple of 16.  A layer's INT8 product, to bf16 or fp32 with a bias, of any K: qm_linear_int8.
  */
 qm_status qm_gemm(const uint8_t* codes_l, int32_t fmt_l, const float* delta_l, int32_t gran_l,
                   const uint8_t* codes_r, int32_t fmt_r, const float* delta_r, int32_t gran_r,
@@ -283,8 +283,9 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
  * The operators of a layer whose projections run in 8 bits, for use with the formats that the probe
  * has found good enough: a norm that leaves codes, and the INT8 product of codes, plain and gated.
  * (The paper's layers quantize what a norm has written and descale into fp32; these
- * calls do the same arithmetic without the tensors in between.)  All three take matrices of any extents and
- * any row pitch; rows that are multiples of 16 bytes, 16-byte aligned, are the fast case.  M or rows may
+ * calls do the same arithmetic without the tensors in between.)  All three take matrices of odd extents and
+ * any row pitch (of codes, multiples of 16 bytes); rows that are multiples of 16 bytes, 16-byte aligned, are the fast case.  M
+ * and rows up to 2^31 - 1025, N and cols below 2^30, pitches below 2^30; more is QM_ERR_UNSUPPORTED.  M or rows may
  * be 0: nothing is done then, and pointers are not looked at.
  *
  * qm_rms_norm_quantize, per row of `cols` elements:
@@ -317,6 +318,8 @@ qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual
  *  out        [M] rows of N values of out_dtype (qm_dtype), ld_out elements apart, apart from the inputs; what lies between
  *             the rows stays as it was
  * A NaN scale gives NaN in its row or column.  Results do not depend on M or on how the work is split.
+ * (qm_gemm with QM_FMT_INT8 and a scale per channel is the same product without bias, to fp32, in batches and with the raw
+ * sums if they are wanted, for K a multiple of 16; this one takes less than half the time for few rows, as much for thousands.)
  * A wait inside the kernel that runs into its time limit leaves NaN in the outputs it could not compute.
  */
 qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_w, int64_t ld_w,

@@ -131,8 +131,11 @@ __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 // ------------------------------------------------------------------ few rows
 // One tile of 128 weight rows x nt rows of x per CTA, or per cluster that splits the contraction.  Roles: warp 0 issues TMA loads into a
 // ring, warp 1 holds tensor memory and issues the MMAs (weights as M, x as N), warps 2..9 are the epilogue.
-// Bound by what reaches an SM from L2, about 64 bytes a clock (18 KB for 128 contraction entries of 16 rows, 32 KB for 128), and where the
-// weights come from HBM by that: 64 x 8192 x 8192 streams its 67 MB in 9.2 of 14.2 us, 7.3 TB/s.  The rest, and most of a small
+// 128 contraction entries take a CTA 200 ns with 16 rows of x (18 KB) and 225 with 128 (32 KB): the round from a full block over four MMAs to
+// its commit, more than the bytes from L2.  Weights that come from HBM bound by that: 64 x 8192 x 8192 streams its 67 MB in 9.2 of
+// 13.9 us with three sets of weights in turn, part of which L2 still holds (hence more than a copy's rate), and takes 14.5 with 470 MB
+// of sets.  All other times here are with weights in L2 as far as they fit; from HBM, 1 row of 4096 x 1024 takes 3.8 us instead of
+// 2.8, of 4096 x 4096 5.5 instead of 4.3.  The rest, and most of a small
 // call (1 x 4096 x 1024 3.1 us): 0.5 to 1.5 us to the first block, 0.2 from the last block to complete accumulators, 0.6 to hand the
 // sums over, 0.4 for the cluster's barrier, 0.2 to 0.8 to finish the rows, 0.3 for the next kernel to start.  Tried: sums read
 // from the peers instead of pushed (+0.7 us), the barrier of the next block asked ahead of this block's MMAs (no
@@ -418,7 +421,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
 // Bound by the tensor cores from contractions of 2048 on (8192 x 8192 x 4096 167 us, 3.3 POP/s; 531 cycles for 128 entries, 512 at the
 // pipe's peak), below that by the output: 16384 x 4096 x 1024 takes 54 us, 44 without its stores, and 35 with a contraction
 // of 128, which is what a fill of those 134 MB takes (34.8).  Bulk stores of the staged rows and plain ones measured the same; four stages
-// 59, cache hints on the stores 53 to 54.  The gated form's epilogue alone (contraction of 128) is 37 us for 8192 x 4096 outputs, half
+// 59, cache hints on the stores 53 to 54.  To fp32 the same product takes 69.5 us (268 MB of output); rows off 16 bytes go out 2 or 4 bytes a
+// lane, one buffer at a time: 6000 x 2603 x 400 35 us.  The gated form's epilogue alone (contraction of 128) is 37 us for 8192 x 4096 outputs, half
 // of it the activation, under 44 of MMAs.
 struct ManyArgs {
   int64_t M, N;
@@ -786,12 +790,14 @@ Scales scales_of(const LinearArgs& l) {
 
 // Which kernel, and how the few rows' one is cut, by the time that it takes: rows of x per tile (nt), parts of the contraction (split),
 // in ns by what was measured on 148 SMs at 1 to 1024 rows, 1024 to 8192 weight rows and contractions of 1024 to 8192:
-//   a CTA of the few rows' kernel: kBase, kDepth for each 128 contraction entries (the MMA warp's issue, not the tensor cores, so that more
+//   a CTA of the few rows' kernel: kBase, kDepth for each 128 contraction entries (the MMA warp's round, so that more
 //   rows cost little), kSplit where sums are exchanged; as often as the CTAs, one to an SM, fill the GPU;
 //   the many rows' kernel: 5000, and for each round of its tiles 310 for 128 contraction entries or the epilogue's 2500, where the output's
 //   rows do not start on 16 bytes 5000 in bf16, 6000 in fp32 and 3600 of the gated form's narrower tiles.
-// What it settles (us, product of 4096 x 4096 weights): 64 rows (nt 64, split 4) 6.6, (64, 1) 9.5, many 13.3; 256 rows (128, 2) 10.0,
-// (64, 2) 16.2, many 13.7; 1024 rows many 15.5, (128, 1) 22.6.
+// Those times are with weights in L2; there is no term for HBM, so that calls that read 60 MB of weights take 3 to 5 us more than it says,
+// whichever cut they get.
+// What it settles (us, product of 4096 x 4096 weights): 64 rows (nt 64, split 4) 6.0, (64, 2) 7.0, (64, 1) 9.3, many 13.2; 256 rows (64, 1) 9.9,
+// which it takes, (128, 2) 9.6, (128, 1) 10.5, (64, 2) 15.4, many 13.7; 1024 rows many 15.0, (128, 1) 21.8.
 struct Plan { int nt, split; };            // nt 0: the many rows' kernel
 Plan make_plan(const LinearArgs& l, bool gated, bool aligned) {
   static constexpr int kNt[4] = {16, 32, 64, 128};
@@ -837,7 +843,9 @@ qm_status launch_few(const LinearArgs& l, const Plan& plan, cudaStream_t s) {
   const size_t blocks = (size_t)((a.num_kb + a.split - 1) / a.split), ring = blocks * stage;
   const bool shortly = ring <= 160 * 1024;
   a.stages = (int)std::min<size_t>({(size_t)kFewStages, blocks, (shortly ? kFewRing / 2 - std::min<size_t>(a.sums_bytes, kFewRing / 4) : kFewRing - a.sums_bytes) / stage});
-  // weights that do not stay in L2 between calls: 24 x 8192 x 4096 gated 14.4 -> 13.9 us; smaller ones lose up to 1 us by it
+  // Weights that do not stay in L2 between the calls of one layer: 24 x 8192 x 4096 gated 14.5 -> 14.0 us.  Smaller ones, when they are there, lose
+  // by it (0.1 to 0.3 us, small calls); when they come from HBM, as those of a deep stack do, they would gain up to 0.7 (1 row of gated 4096 x
+  // 1024 4.8 us, 4.1 with four blocks; of 4096 x 4096 none).
   a.prefetch = (GATED ? 2 : 1) * l.N * l.K >= (32ll << 20) ? 4 : 0;
   a.tiles_m = (int)tiles_m;
   a.idesc = make_idesc(2, 1, 1, kBlock, (uint32_t)a.nt);                      // s8 x s8 -> s32
