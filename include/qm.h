@@ -300,8 +300,8 @@ qm_status qm_gemm_ref(const void* l_bf16, const void* r_bf16, int64_t M, int64_t
  *  weight     `cols` values, bf16 or fp32 (`weight_dtype`).
  *  eps        positive and normal in fp32.
  *  codes      [rows][qm_code_ld(cols)], 16-byte aligned, padding zero;  delta [rows] fp32.
- * A row whose v is all zero gets delta = 1, and so does, with codes 0, one so small that d is 0 in fp32.  A row with a NaN or Inf in z or v (0 times an Inf among the weights is one), or whose sum
- * of squares leaves fp32, gets delta = NaN and codes 0; other rows are as they would be without it.
+ * A row whose v is all zero gets delta = 1, and so does, with codes 0, one so small that d is 0 in fp32.  A row with a NaN or Inf
+ * in z or v (0 times an Inf among the weights is one), or whose sum of squares leaves fp32, gets delta = NaN and codes 0; other rows are as they would be without it.
  */
 qm_status qm_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int32_t dtype,
                                const void* weight, int32_t weight_dtype, float eps, int64_t rows, int64_t cols,
@@ -329,11 +329,13 @@ qm_status qm_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delt
 /*
  * qm_gated_linear_int8: h = act(g) * u with g = x . gate^T and u = x . up^T as in qm_linear_int8 (no bias), both
  * products, the activation (qm_act) and the multiplication in one kernel; g and u are not written.  codes_gate and codes_up may be
- * two halves of one tensor.  act(g) is evaluated in fp32 by approximate exponentials and reciprocals.  In units of 2^-24 it is off by at
- * most 12 |act(g)| (SiLU), (6 |t| + 12) |act(g)| (GELU_TANH, t = 2 sqrt(2/pi) (g + 0.044715 g^3)) and |act(g)| + (1.2 g^2 + 22) |g| Phi(-|g|)
- * (GELU, Phi the normal law's integral), where the output is bf16 (1.3 |g| + 24) |act(g)| and (7.3 |t| + 24) |act(g)| for the
- * first two; what is below fp32's normal numbers may come out as 0 (of either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times
- * Inf).  Other arguments as for qm_linear_int8.
+ * two halves of one tensor.  act(g) is evaluated in fp32 by approximate exponentials and reciprocals.  In units of 2^-24 it is off by at most
+ *   QM_ACT_SILU       12 |act(g)|              (out_dtype bf16: (1.3 |g| + 24) |act(g)|)
+ *   QM_ACT_GELU_TANH  (6 |t| + 12) |act(g)|    (bf16: (7.3 |t| + 24) |act(g)|), t = 2 sqrt(2/pi) (g + 0.044715 g^3)
+ *   QM_ACT_GELU       |act(g)| + (1.2 g^2 + 22) |g| Phi(-|g|), Phi the normal law's integral
+ * and, where act(g) nears the end of fp32's normal numbers, by 2^-139 (QM_ACT_GELU: 2^-125) besides; what is below them may come out
+ * as 0 (of either sign).  A gate beyond fp32 gives what the formulas give: act(+Inf) = +Inf, act(-Inf) = NaN (0 times Inf).
+ * Other arguments as for qm_linear_int8.
  */
 qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float* delta_x, const uint8_t* codes_gate,
                                int64_t ld_gate, const float* delta_gate, const uint8_t* codes_up, int64_t ld_up,
