@@ -343,6 +343,39 @@ qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float
                                int32_t out_dtype, int64_t ld_out, void* stream);
 
 /*
+ * FP8 with a scale for each 128 entries of the contraction (QM_SCALE_BLOCK), where one scale for a whole row is too coarse: the codes
+ * of a matrix, and the product of two such matrices.  Scales lie block of the contraction outermost: delta[c * R + r] with
+ * c = k / 128 and R the number of blocks of rows.
+ *
+ * qm_quantize_blocks: Eq. 1 over each block of `side` rows (non-contracting indices; 1 or 128, the last block may be smaller) and 128 contraction
+ * entries: delta = max|x| / qmax, codes = sat(RTNE(x / delta)) as qm_quantize gives them under that scale.
+ *  x          a 2-D operand (batch 1), either dimension contiguous, bf16 or fp32
+ *  fmt        QM_FMT_E4M3 or QM_FMT_E5M2
+ *  delta      device fp32 [ceil(contract / 128)][ceil(noncontract / side)]
+ *  codes      device bytes [noncontract][qm_code_ld(contract)], the contracting index contiguous, padding zero, 16-byte aligned
+ * A block of zeros gets delta = 1, and so does, with codes 0, one so small that delta is 0 in fp32.  One with a NaN or Inf gets delta = NaN and codes 0.
+ * The codes of a weight for forward and input gradient are two calls, one for each orientation; side = 128 gives both the same scales.
+ */
+#define QM_SCALE_BLOCK 128
+qm_status qm_quantize_blocks(const qm_operand* x, int32_t fmt, int32_t side, float* delta, uint8_t* codes, void* stream);
+
+/*
+ * qm_linear_fp8: y_ij = sum over blocks c of (dx[c][i] * dw[c][j / side_w]) * (sum over the k of c of x_ik w_jk), + bias[j].  The inner sums are the
+ * tensor cores' (fp32), the outer one is fp32, rounded once to the output's type.  Forward: x activations, w weights with side_w = 128;
+ * input gradient: x the output's gradient, w the weight's codes of the other orientation; weight gradient: both operands with the
+ * tokens as their contraction and side_w = 1.
+ *  codes_x    [M] rows of K FP8 codes of fmt_x, ld_x bytes apart;  delta_x [ceil(K / 128)][M], a scale per row and block
+ *  codes_w    [N] rows of K codes of fmt_w, ld_w bytes apart;       delta_w [ceil(K / 128)][ceil(N / side_w)], side_w 1 or 128
+ *             (both 16-byte aligned, pitches multiples of 16, e.g. qm_code_ld(K); bytes from K on are not looked at)
+ *  bias, out and the limits of M, N and the pitches as for qm_linear_int8; K below 2^30.  M may be 0.
+ * A NaN scale gives NaN in its row, or its side_w columns.  The same call gives the same bits each time; another M or N may add the blocks in another order.
+ * A wait inside the kernel that runs into its time limit leaves NaN in the outputs it could not compute.
+ */
+qm_status qm_linear_fp8(const uint8_t* codes_x, int64_t ld_x, int32_t fmt_x, const float* delta_x, const uint8_t* codes_w, int64_t ld_w,
+                        int32_t fmt_w, const float* delta_w, int32_t side_w, const void* bias, int32_t bias_dtype, int64_t M, int64_t N,
+                        int64_t K, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
+
+/*
  * Eq. 3 on materialised arrays: ref = C, q = Q, den = D, each `count` fp32
  * values.  `out` receives the record: device memory, or pinned host memory,
  * which the call's last kernel stores to directly, every field once and none

@@ -108,6 +108,8 @@ def lib():
             "qm_rms_norm_quantize": (I32, [P, I64, P, I64, I32, P, I32, C.c_float, I64, I64, I32, P, I64, P, P, P]),
             "qm_linear_int8": (I32, [P, I64, P, P, I64, P, P, I32, I64, I64, I64, P, I32, I64, P]),
             "qm_gated_linear_int8": (I32, [P, I64, P, P, I64, P, P, I64, P, I32, I64, I64, I64, P, I32, I64, P]),
+            "qm_quantize_blocks": (I32, [OP, I32, I32, P, P, P]),
+            "qm_linear_fp8": (I32, [P, I64, I32, P, P, I64, I32, P, I32, P, I32, I64, I64, I64, P, I32, I64, P]),
             "qm_metric_workspace_bytes": (SZ, [I64]),
             "qm_metric": (I32, [P, P, P, I64, P, P, SZ, P]),
             "qm_metric_scalars": (I32, [C.POINTER(MetricResult), C.POINTER(MetricScalars)]),
@@ -402,6 +404,51 @@ def qm_gated_linear_int8(codes_x, delta_x, codes_gate, delta_gate, codes_up, del
                                     ACT[act], M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
     if st:
         _check(st, "qm_gated_linear_int8")
+    return out
+
+
+SCALE_BLOCK = 128                    # contraction entries under one scale of qm_quantize_blocks and qm_linear_fp8
+
+
+def _blocks(n, side=SCALE_BLOCK):
+    return (n + side - 1) // side
+
+
+def qm_quantize_blocks(op, fmt, side=1, stream=None):
+    """FP8 codes of a 2-D operand with a scale for each 128 contraction entries of `side` rows (1 or 128):
+    (codes [rows, qm_code_ld(K)], delta [ceil(K / 128), ceil(rows / side)]), as qm_linear_fp8 takes them."""
+    device, handle = _on(stream)
+    if side not in (1, SCALE_BLOCK):
+        _refuse(f"side: 1 or {SCALE_BLOCK}")
+    t = op._keep
+    if t.get_device() != device:
+        _refuse("operand: wants a tensor on the current CUDA device")
+    codes = _new(t, (op.noncontract, qm_code_ld(op.contract)), torch.uint8, stream)
+    delta = _new(t, (_blocks(op.contract), _blocks(op.noncontract, side)), torch.float32, stream)
+    st = lib().qm_quantize_blocks(C.byref(op), FMT[fmt], side, delta.data_ptr(), codes.data_ptr(), handle)
+    if st:
+        _check(st, "qm_quantize_blocks")
+    return codes, delta
+
+
+def qm_linear_fp8(codes_x, delta_x, codes_w, delta_w, K, fmt_x="e4m3", fmt_w="e4m3", side_w=SCALE_BLOCK, bias=None, out_dtype=torch.bfloat16,
+                  out=None, stream=None):
+    """FP8 product with a scale for each 128 contraction entries -> [M, N] in bf16 or fp32.  codes_x [M, >= K] with delta_x
+    [ceil(K / 128), M] and codes_w [N, >= K] with delta_w [ceil(K / 128), ceil(N / side_w)] are what qm_quantize_blocks leaves with side = 1 and
+    side = side_w; other arguments as for qm_linear_int8."""
+    device, handle = _on(stream)
+    if side_w not in (1, SCALE_BLOCK):
+        _refuse(f"side_w: 1 or {SCALE_BLOCK}")
+    M, ld_x = _codes(codes_x, "codes_x", K, device)
+    N, ld_w = _codes(codes_w, "codes_w", K, device)
+    dx = _vector(delta_x, "delta_x", _blocks(K) * M, _FP32, device)
+    dw = _vector(delta_w, "delta_w", _blocks(K) * _blocks(N, side_w), _FP32, device)
+    b = _vector(bias, "bias", N, _FLOATS, device) if bias is not None else None
+    out, ld = _linear_out(out, out_dtype, M, N, codes_x, stream, device)
+    st = lib().qm_linear_fp8(codes_x.data_ptr(), ld_x, FMT[fmt_x], dx, codes_w.data_ptr(), ld_w, FMT[fmt_w], dw, side_w, b,
+                             _DT[bias.dtype] if b is not None else 0, M, N, K, out.data_ptr(), _DT[out.dtype], ld, handle)
+    if st:
+        _check(st, "qm_linear_fp8")
     return out
 
 

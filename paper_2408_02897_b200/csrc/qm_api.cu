@@ -448,6 +448,41 @@ qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float
   return run_linear(a, static_cast<cudaStream_t>(stream));
 }
 
+qm_status qm_quantize_blocks(const qm_operand* x, int32_t fmt, int32_t side, float* delta, uint8_t* codes, void* stream) {
+  View v;
+  const qm_status st = to_view(x, &v);
+  if (st != QM_OK) return st;
+  if (!valid_fmt(fmt) || (side != 1 && side != kScaleBlock) || !delta || !codes) return QM_ERR_INVALID_ARG;
+  if (fmt == QM_FMT_INT8 || v.batch != 1 || !sane(v.nc) || v.c >= (1ll << 30)) return QM_ERR_UNSUPPORTED;
+  if (addr(codes) % 16 || addr(delta) % 4) return QM_ERR_ALIGNMENT;
+  return launch_quantize_blocks(v, fmt, side, delta, codes, static_cast<cudaStream_t>(stream));
+}
+
+qm_status qm_linear_fp8(const uint8_t* codes_x, int64_t ld_x, int32_t fmt_x, const float* delta_x, const uint8_t* codes_w, int64_t ld_w,
+                        int32_t fmt_w, const float* delta_w, int32_t side_w, const void* bias, int32_t bias_dtype, int64_t M, int64_t N,
+                        int64_t K, void* out, int32_t out_dtype, int64_t ld_out, void* stream) {
+  if (M < 0 || N <= 0 || K <= 0 || !valid_dtype(out_dtype) || (bias && !valid_dtype(bias_dtype))) return QM_ERR_INVALID_ARG;
+  if (!valid_fmt(fmt_x) || !valid_fmt(fmt_w) || (side_w != 1 && side_w != kScaleBlock)) return QM_ERR_INVALID_ARG;
+  if (fmt_x == QM_FMT_INT8 || fmt_w == QM_FMT_INT8) return QM_ERR_UNSUPPORTED;
+  if (M == 0) return QM_OK;
+  if (!codes_x || !delta_x || !codes_w || !delta_w || !out) return QM_ERR_INVALID_ARG;
+  if ((N > 1 && ld_w < K) || (M > 1 && (ld_x < K || ld_out < N))) return QM_ERR_INVALID_ARG;
+  // the pitch of a single row carries no information: give it the dense value
+  if (M == 1) { ld_x = qm_code_ld(K); ld_out = N; }
+  if (N == 1) ld_w = qm_code_ld(K);
+  if (!sane(M) || N >= (1ll << 30) || K >= (1ll << 30) || !sane_pitch(ld_x) || !sane_pitch(ld_w) || !sane_pitch(ld_out)) return QM_ERR_UNSUPPORTED;
+  if (addr(codes_x) % 16 || ld_x % 16 || addr(codes_w) % 16 || ld_w % 16 || addr(delta_x) % 4 || addr(delta_w) % 4 ||
+      addr(out) % elem_bytes(out_dtype) || (bias && addr(bias) % elem_bytes(bias_dtype)))
+    return QM_ERR_ALIGNMENT;
+  LinearFp8Args a{};
+  a.x = codes_x; a.ld_x = ld_x; a.fmt_x = fmt_x; a.dx = delta_x;
+  a.w = codes_w; a.ld_w = ld_w; a.fmt_w = fmt_w; a.dw = delta_w; a.side_w = side_w;
+  a.bias = bias; a.bias_dtype = bias_dtype;
+  a.M = M; a.N = N; a.K = K;
+  a.out = out; a.out_dtype = out_dtype; a.ld_out = ld_out;
+  return launch_linear_fp8(a, static_cast<cudaStream_t>(stream));
+}
+
 size_t qm_metric_workspace_bytes(int64_t count) {
   if (count <= 0) return 0;
   return align256(sizeof(double) * kPartialDoubles * (size_t)metric_blocks(count));

@@ -168,6 +168,19 @@ struct LinearArgs {
 };
 qm_status launch_linear_int8(const LinearArgs& a, cudaStream_t s);
 
+// ---- FP8 codes with a scale for each block, and their product (quantize_blocks.cu, linear_fp8.cu) ----
+// side: rows under one scale, 1 or 128.  codes: rows of qm_code_ld(x.c) bytes.
+constexpr int kScaleBlock = 128;            // contraction entries under one scale
+qm_status launch_quantize_blocks(const View& x, int fmt, int side, float* delta, uint8_t* codes, cudaStream_t s);
+struct LinearFp8Args {
+  const uint8_t* x; int64_t ld_x; int fmt_x; const float* dx;
+  const uint8_t* w; int64_t ld_w; int fmt_w; const float* dw; int side_w;
+  const void* bias; int bias_dtype;
+  int64_t M, N, K;
+  void* out; int out_dtype; int64_t ld_out;
+};
+qm_status launch_linear_fp8(const LinearFp8Args& a, cudaStream_t s);
+
 // ---- metric (metric.cu) ----------------------------------------------------
 // One partial record per CTA: {sum_be, max_be, sum_diff2, sum_ref2, sum_den2} as doubles.
 constexpr int kPartialDoubles = 5;

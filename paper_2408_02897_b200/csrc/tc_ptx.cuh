@@ -196,6 +196,11 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// What a wait has brought, said to the compiler: nothing that uses it moves ahead of the wait.
+__device__ __forceinline__ void landed(uint32_t (&r)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]));
+}
 
 // Instruction descriptor: D format [4,6), A format [7,10), B format [10,13), majors [15],[16]
 // (0 = contraction-major), N/8 at [17,23), M/16 at [24,29).
@@ -277,6 +282,13 @@ __device__ __forceinline__ void mma_i8_one(uint32_t tmem_d, uint64_t da, uint64_
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The same in FP8, fp32 sums.
+__device__ __forceinline__ void mma_f8_one(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tc_commit_one(uint32_t bar) {
