@@ -376,6 +376,62 @@ qm_status qm_linear_fp8(const uint8_t* codes_x, int64_t ld_x, int32_t fmt_x, con
                         int64_t K, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
 
 /*
+ * A cache of keys and values in 8 bits, with a scale for each block of tokens and head, and the attention that reads it.
+ *  k_codes, v_codes   device bytes [blocks][kv_heads][block_tokens][head_dim], 16-byte aligned
+ *  k_delta, v_delta   device fp32 [blocks][kv_heads]: code * delta stands for the value
+ *  tables             device int32 [batch] rows, ld_tables apart, of table_width block numbers: position p of sequence b lies in block
+ *                     tables[b][p / block_tokens], slot p % block_tokens.  Entries beyond a sequence's length are not looked at.
+ *  lens               device int32 [batch]: the sequences' lengths, the new tokens included, as both calls below want them
+ *  starts             device int32 [batch + 1]: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1 of k, v and q, its last tokens in
+ *                     that order; a sequence may have none.  NULL: one for each sequence (tokens = batch).
+ *  fmt                qm_format, of keys and values alike
+ * block_tokens is a power of two from 16 to 256, head_dim a multiple of 16 up to 128.  A block must not be in two places of the tables if one of
+ * them is written.  Scales are at least 0; one below 2^-60 counts as 0.  What tables, lens and starts say is checked on the device: a
+ * sequence whose rows of `starts` are not inside 0 .. tokens has no new tokens, a position below 0 does not exist, and no block
+ * outside 0 .. blocks - 1 or beyond the table is touched.
+ */
+typedef struct {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* k_delta;
+  float* v_delta;
+  int64_t blocks;
+  int32_t kv_heads, block_tokens, head_dim, fmt;
+  const int32_t* tables;
+  int64_t ld_tables;
+  int32_t table_width, batch;
+  const int32_t* lens;
+  const int32_t* starts;
+} qm_cache;
+
+/*
+ * qm_cache_append: puts the new tokens into the cache.  For each block and head that gets some, delta = max(the scale of what the block holds
+ * already, max|new| / qmax); if that is larger than before, the codes that it holds become sat(RTNE((code * old) / delta)), and new codes
+ * are sat(RTNE(x / delta)), all of it in fp32 as in qm_quantize.  What is held is what lies in the slots before the first new token's: a block whose
+ * slot 0 is written starts anew, whatever was in it.  (Unlike Eq. 1's, the scale of nothing but zeros is 0: it would keep
+ * later tokens from their own.)  A NaN or Inf makes the block's scale NaN for as long as it is held, with codes 0 for the tokens that come with or after it.
+ *  k, v     [tokens][kv_heads][head_dim] of dtype (bf16 or fp32), tokens ld_* elements apart; 16-byte aligned, ld_* a multiple of 8
+ * tokens may be 0.  Tokens of a position that has no block are not stored.
+ */
+qm_status qm_cache_append(const qm_cache* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int32_t dtype, int64_t tokens,
+                          void* stream);
+
+/*
+ * qm_cache_attention: out = softmax(scale * q . k^T) . v for the new tokens, each over the keys up to and with its own position.
+ *  q        bf16 [tokens][heads][head_dim], tokens ld_q elements apart; query head h reads cached head h / (heads / kv_heads)
+ *  out      bf16, the same shape, ld_out apart;  q and out 16-byte aligned, ld_* multiples of 8
+ *  lse      optional (NULL) fp32 [tokens][heads]: log sum exp(scale * q . k), natural
+ *  ws       device scratch of at least qm_cache_attention_workspace_bytes(head_dim) bytes, 256-byte aligned; its contents do not matter and
+ *           concurrent calls must not share it (nor two captured graphs that may run at the same time)
+ * A token whose position is below 0 sees nothing: out 0, lse -inf.  One that sees a token of a block with a NaN scale, or of a
+ * position that has no block, gets NaN.  Codes of tokens that nothing new sees, and their scales, may be anything.  The weights are rounded to fp16's 11 bits ahead of their
+ * product with the values; scores, statistics and sums are fp32.  The same call gives the same bits each time.
+ */
+size_t qm_cache_attention_workspace_bytes(int32_t head_dim);
+qm_status qm_cache_attention(const qm_cache* cache, const void* q, int64_t ld_q, int32_t heads, float scale, int64_t tokens, void* out,
+                             int64_t ld_out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Eq. 3 on materialised arrays: ref = C, q = Q, den = D, each `count` fp32
  * values.  `out` receives the record: device memory, or pinned host memory,
  * which the call's last kernel stores to directly, every field once and none

@@ -84,6 +84,12 @@ class ProbeCfg(C.Structure):
                 ("batch_groups_l", C.c_int32), ("batch_groups_r", C.c_int32), ("row_stats", C.c_void_p)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_delta", C.c_void_p), ("v_delta", C.c_void_p), ("blocks", C.c_int64),
+                ("kv_heads", C.c_int32), ("block_tokens", C.c_int32), ("head_dim", C.c_int32), ("fmt", C.c_int32), ("tables", C.c_void_p),
+                ("ld_tables", C.c_int64), ("table_width", C.c_int32), ("batch", C.c_int32), ("lens", C.c_void_p), ("starts", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -110,6 +116,9 @@ def lib():
             "qm_gated_linear_int8": (I32, [P, I64, P, P, I64, P, P, I64, P, I32, I64, I64, I64, P, I32, I64, P]),
             "qm_quantize_blocks": (I32, [OP, I32, I32, P, P, P]),
             "qm_linear_fp8": (I32, [P, I64, I32, P, P, I64, I32, P, I32, P, I32, I64, I64, I64, P, I32, I64, P]),
+            "qm_cache_append": (I32, [C.POINTER(Cache), P, I64, P, I64, I32, I64, P]),
+            "qm_cache_attention_workspace_bytes": (SZ, [I32]),
+            "qm_cache_attention": (I32, [C.POINTER(Cache), P, I64, I32, C.c_float, I64, P, I64, P, P, SZ, P]),
             "qm_metric_workspace_bytes": (SZ, [I64]),
             "qm_metric": (I32, [P, P, P, I64, P, P, SZ, P]),
             "qm_metric_scalars": (I32, [C.POINTER(MetricResult), C.POINTER(MetricScalars)]),
@@ -450,6 +459,78 @@ def qm_linear_fp8(codes_x, delta_x, codes_w, delta_w, K, fmt_x="e4m3", fmt_w="e4
     if st:
         _check(st, "qm_linear_fp8")
     return out
+
+
+_INTS = (torch.int32,)
+
+
+def _cache(k_codes, k_delta, v_codes, v_delta, tables, lens, starts, fmt, device):
+    """A cache that is described by its tensors, as the library takes it."""
+    shape = k_codes.shape
+    if len(shape) != 4 or v_codes.shape != shape:
+        _refuse("k_codes and v_codes: want [blocks, kv_heads, block_tokens, head_dim] both")
+    blocks, kv_heads, block_tokens, dim = shape
+    n = blocks * kv_heads * block_tokens * dim
+    batch, width, ld = _matrix(tables, "tables", _INTS, device)
+    return Cache(_vector(k_codes, "k_codes", n, _BYTES, device), _vector(v_codes, "v_codes", n, _BYTES, device),
+                 _vector(k_delta, "k_delta", blocks * kv_heads, _FP32, device), _vector(v_delta, "v_delta", blocks * kv_heads, _FP32, device),
+                 blocks, kv_heads, block_tokens, dim, FMT[fmt], tables.data_ptr(), ld, width, batch,
+                 _vector(lens, "lens", batch, _INTS, device),
+                 _vector(starts, "starts", batch + 1, _INTS, device) if starts is not None else None)
+
+
+def _token_rows(t, what, heads, dim, dtypes, device):
+    """(tokens, heads, pitch) of [tokens, heads, dim] with contiguous tokens of any pitch."""
+    if t.dtype not in dtypes or t.get_device() != device or t.dim() != 3:
+        _refuse(f"{what}: wants a 3-D {' or '.join(map(str, dtypes))} tensor on the current CUDA device")
+    tokens, h, d = t.shape
+    pitch, step, unit = t.stride()
+    if (heads is not None and h != heads) or d != dim:
+        _refuse(f"{what}: wants [tokens, {'heads' if heads is None else heads}, {dim}]")
+    if (unit != 1 and d > 1) or (step != d and h > 1):
+        _refuse(f"{what}: the heads of a token must be contiguous")
+    return tokens, h, pitch if tokens > 1 else h * d
+
+
+def qm_cache_append(k, v, k_codes, k_delta, v_codes, v_delta, tables, lens, starts=None, fmt="int8", stream=None):
+    """Puts new tokens k, v [tokens, kv_heads, head_dim] (any pitch between tokens) into an 8-bit cache with a scale for each block of
+    tokens and head, in place: codes [blocks, kv_heads, block_tokens, head_dim] (uint8) and scales [blocks, kv_heads].  tables
+    [batch, width] (int32) names the blocks of each sequence, lens [batch] its length with the new tokens, starts [batch + 1] its rows of
+    k and v (None: one token for each sequence)."""
+    device, handle = _on(stream)
+    cache = _cache(k_codes, k_delta, v_codes, v_delta, tables, lens, starts, fmt, device)
+    tokens, _, ld_k = _token_rows(k, "k", cache.kv_heads, cache.head_dim, _FLOATS, device)
+    v_tokens, _, ld_v = _token_rows(v, "v", cache.kv_heads, cache.head_dim, (k.dtype,), device)
+    if v_tokens != tokens:
+        _refuse("k and v differ in their number of tokens")
+    st = lib().qm_cache_append(C.byref(cache), k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[k.dtype], tokens, handle)
+    if st:
+        _check(st, "qm_cache_append")
+
+
+def qm_cache_attention(q, k_codes, k_delta, v_codes, v_delta, tables, lens, starts=None, fmt="int8", scale=None, out=None, want_lse=False,
+                       stream=None):
+    """Attention of new tokens q [tokens, heads, head_dim] (bf16, any pitch between tokens) over the cache that qm_cache_append fills, each
+    over the keys up to its own position: (out [tokens, heads, head_dim] bf16, log-sum-exp [tokens, heads] fp32 or None).  heads is a
+    multiple of the cache's; scale None: head_dim ** -0.5.  The cache, lens (with the new tokens) and starts as for qm_cache_append."""
+    device, handle = _on(stream)
+    cache = _cache(k_codes, k_delta, v_codes, v_delta, tables, lens, starts, fmt, device)
+    dim = cache.head_dim
+    tokens, heads, ld_q = _token_rows(q, "q", None, dim, (torch.bfloat16,), device)
+    if out is None:
+        out = _new(q, (tokens, heads, dim), torch.bfloat16, stream)
+    o_tokens, _, ld_out = _token_rows(out, "out", heads, dim, (torch.bfloat16,), device)
+    if o_tokens != tokens:
+        _refuse("q and out differ in their number of tokens")
+    lse = _new(q, (tokens, heads), torch.float32, stream) if want_lse else None
+    L = lib()
+    n = L.qm_cache_attention_workspace_bytes(dim)
+    ws = _new(q, (n,), torch.uint8, stream)
+    st = L.qm_cache_attention(C.byref(cache), q.data_ptr(), ld_q, heads, dim ** -0.5 if scale is None else scale, tokens, out.data_ptr(), ld_out,
+                              lse.data_ptr() if want_lse else None, ws.data_ptr(), n, handle)
+    if st:
+        _check(st, "qm_cache_attention")
+    return out, lse
 
 
 def _read_result(dev_buf):

@@ -1,0 +1,144 @@
+// New keys and values into the 8-bit cache (qm_cache_append).
+//
+// A block of tokens and a head have one scale, delta = max|x| / qmax over what the block has held; where new tokens raise it, the
+// codes that are there already are rounded again under the new one.  One unit of work is a touched block, a head, and keys or values: it
+// finds the new tokens' maximum, then writes codes.  Bound by HBM for prompts (the new tokens are read once from there and once
+// from L1 or L2), by latency for a token at a time.
+#include "cache_device.cuh"
+
+namespace qm {
+namespace {
+
+struct AppendArgs {
+  CacheView c;
+  const void *k, *v;
+  int64_t ld_k, ld_v;              // elements between tokens
+  int64_t units;                   // (block, head)
+};
+
+template <int FMT>
+__device__ __noinline__ uint32_t append_far(float x0, float x1, float delta) {
+  const Quotient quot(delta);
+  return quant2<FMT>(quot(x0), quot(x1));
+}
+// Two codes under a scale that covers both magnitudes.
+template <int FMT>
+__device__ __forceinline__ uint32_t append_pair(float x0, float x1, float delta, const QuotientPair& quot) {
+  if (QuotientPair::serves(delta)) return quant_pair_x2<FMT>(x0, x1, quot);
+  return delta > 0.f && delta < INFINITY ? append_far<FMT>(x0, x1, delta) & 0xffffu : 0u;
+}
+template <int FMT>
+__device__ __forceinline__ uint2 append8(const Vec8& v, float delta, const QuotientPair& quot) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = append_pair<FMT>(v.v[2 * i], v.v[2 * i + 1], delta, quot);
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t again4(uint32_t codes, float before, float after, const QuotientPair& quot) {
+  uint32_t h[2];
+  half4_of<FMT>(codes, h[0], h[1]);
+  uint32_t r[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    r[i] = append_pair<FMT>(f.x * before, f.y * before, after, quot);
+  }
+  return r[0] | r[1] << 16;
+}
+
+// THREADS: to a unit, 32 or 128 (of which a thread block has four, or one).
+template <typename T, int FMT, int THREADS>
+__global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
+  pdl_prologue();
+  const CacheView& c = a.c;
+  const int64_t unit = (int64_t)blockIdx.x * (128 / THREADS) + threadIdx.x / THREADS;
+  if (unit >= a.units) return;
+  const int tid = threadIdx.x % THREADS, head = (int)(unit % c.kv_heads);
+  const int64_t cand = unit / c.kv_heads;
+  // Sequence b has the candidates from starts[b] / block_tokens + 2 b on, at least as many as the blocks that it touches.
+  int lo = 0, hi = c.batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    const int64_t from = ((c.starts ? c.starts[mid] : mid) >> c.shift) + 2ll * mid;
+    if (from <= cand) lo = mid; else hi = mid - 1;
+  }
+  const int b = lo;
+  const int64_t j = cand - ((c.starts ? c.starts[b] : b) >> c.shift) - 2ll * b;
+  const Extent e = extent_of(c, b);
+  const int64_t p0 = max((int64_t)e.len - e.n, (int64_t)0);                  // position of the first new token (those before 0 have none)
+  const int64_t block = (p0 >> c.shift) + j;
+  if (e.n == 0 || j < 0 || block > ((int64_t)e.len - 1) >> c.shift || e.len == 0) return;
+  const int64_t from = max(p0, block << c.shift), to = min((int64_t)e.len, (block + 1) << c.shift);
+  const int page = page_of(c, b, (int)block);
+  if (page < 0) return;
+  const int slot = (int)(from & ((1 << c.shift) - 1)), n = (int)(to - from);
+  const int64_t token = e.first + (from - ((int64_t)e.len - e.n));
+
+  const bool values = blockIdx.y;
+  const T* const x = static_cast<const T*>(values ? a.v : a.k) + token * (values ? a.ld_v : a.ld_k) + (int64_t)head * c.dim;
+  const int64_t ld = values ? a.ld_v : a.ld_k;
+  const int64_t at = (int64_t)page * c.kv_heads + head;
+  uint8_t* const codes = (values ? c.v : c.k) + (at << c.shift) * c.dim;
+  float* const delta = (values ? c.dv : c.dk) + at;
+  const int per = c.dim / 8, work = n * per;                                 // eight elements at a time
+
+  uint32_t top = 0;
+#pragma unroll 4
+  for (int i = tid; i < work; i += THREADS) top = absmax8(Loader<T>::load8(x + (int64_t)(i / per) * ld + i % per * 8), top);
+  const float before = slot ? *delta : 0.f;
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (THREADS > 32) {
+    __shared__ uint32_t tops[4];
+    if ((tid & 31) == 0) tops[tid >> 5] = top;
+    __syncthreads();                                                         // (and all have read the old scale)
+    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  }
+  float after = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : __fdiv_rn(__uint_as_float(top), fmt_qmax(FMT));
+  if (after < kLeastScale) after = 0.f;
+  after = before > after || before != before ? before : after;
+  const QuotientPair quot(after);
+  __syncwarp();
+  if (tid == 0) *delta = after;
+  if (slot && after > before) {
+    for (int i = tid; i < slot * c.dim / 16; i += THREADS) {
+      uint4 w = reinterpret_cast<uint4*>(codes)[i];
+      w.x = again4<FMT>(w.x, before, after, quot); w.y = again4<FMT>(w.y, before, after, quot);
+      w.z = again4<FMT>(w.z, before, after, quot); w.w = again4<FMT>(w.w, before, after, quot);
+      reinterpret_cast<uint4*>(codes)[i] = w;
+    }
+  }
+#pragma unroll 4
+  for (int i = tid; i < work; i += THREADS)
+    *reinterpret_cast<uint2*>(codes + (int64_t)slot * c.dim + i * 8) =
+        append8<FMT>(Loader<T>::load8(x + (int64_t)(i / per) * ld + i % per * 8), after, quot);
+}
+
+template <typename T, int FMT>
+qm_status launch_typed(const AppendArgs& a, cudaStream_t s) {
+  // a warp where a unit has a token or two, as when one is generated at a time
+  if (a.c.tokens <= 2ll * a.c.batch) {
+    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 32>, dim3((unsigned)((a.units + 3) / 4), 2), dim3(128), 0, s, a));
+  } else {
+    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 128>, dim3((unsigned)a.units, 2), dim3(128), 0, s, a));
+  }
+  count_launch();
+  return QM_OK;
+}
+template <typename T>
+qm_status launch_format(const AppendArgs& a, int fmt, cudaStream_t s) {
+  return fmt == QM_FMT_INT8 ? launch_typed<T, QM_FMT_INT8>(a, s) : fmt == QM_FMT_E4M3 ? launch_typed<T, QM_FMT_E4M3>(a, s) : launch_typed<T, QM_FMT_E5M2>(a, s);
+}
+
+}  // namespace
+
+qm_status launch_cache_append(const CacheArgs& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, cudaStream_t s) {
+  AppendArgs a{};
+  a.c = view_of(c);
+  a.k = k; a.v = v; a.ld_k = ld_k; a.ld_v = ld_v;
+  a.units = ((c.tokens >> a.c.shift) + 2 * c.batch) * c.kv_heads;
+  if (a.units >= (1ll << 31)) return QM_ERR_UNSUPPORTED;
+  return dtype == QM_DT_BF16 ? launch_format<__nv_bfloat16>(a, c.fmt, s) : launch_format<float>(a, c.fmt, s);
+}
+
+}  // namespace qm

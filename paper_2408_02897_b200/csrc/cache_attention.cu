@@ -1,0 +1,446 @@
+// Attention over the 8-bit cache (qm_cache_attention).
+//
+//   x_ij = scale q_i . (dk k_j),   o_i = sum_j p_ij (dv v_j) / sum_j p_ij,   p_ij = exp(x_ij - max), j up to the position of i
+// in one pass over the keys, with a running maximum. dk and dv are one number for a block of tokens: dk goes into the score. dv goes into
+// the exponent: with x'_ij = x_ij log2 e + log2 dv and M its running maximum, P_ij = 2^(x'_ij - M) is what is rounded to fp16 and multiplied
+// with the codes, and the denominator adds P_ij / dv: both are relative to the same maximum, o_i = sum P_ij v_j / sum (P_ij / dv), and no block's
+// codes are scaled. Codes are exact in fp16 (8 bits or less of significand), queries too under a power of two for each row; products are
+// exact in the tensor cores' fp32 sums, P has 11 bits (2^14 is its largest value, so that 2^-28 of it is still a normal number), the
+// statistics and both sums are fp32.
+//
+// attention_rows: 16 query rows (tokens x query heads of one cached head) at a time against all keys, mma.sync m16n8k16 from registers: a
+// thread loads 16 bytes of keys or values straight from the cache in the places that the instruction's operands have, so nothing goes through
+// shared memory. A thread block takes an equal share of the cells (32 tokens for 16 rows and a head) of all sequences together, wherever they begin
+// and end; what is left of rows whose keys were shared out is joined by attention_join, in the order of the keys.
+#include <algorithm>
+#include <atomic>
+
+#include "cache_device.cuh"
+
+namespace qm {
+namespace {
+
+constexpr int kWarps = 8, kRows = 16, kCell = 32;
+constexpr int kMaxBlocks = 512;                 // of a launch
+
+struct RowsArgs {
+  CacheView c;
+  const __nv_bfloat16* q; int64_t ld_q;
+  int heads, group;                              // group: query heads of a cached head
+  float scale_log2;                              // of scores to the base 2
+  __nv_bfloat16* out; int64_t ld_out;
+  float* lse;
+  struct Share* shares;                          // one a thread block
+  float* parts;                                  // [2 * blocks][16][padded dim + 2]
+};
+
+// Where a thread block's share of the cells begins, and the rows that it begins in.
+struct Share { int64_t lo, start, end; int b, item; };
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <int N> struct Words { uint32_t w[N]; };
+__device__ __forceinline__ Words<4> load_words(const uint8_t* p, Words<4>) {
+  Words<4> r;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ Words<2> load_words(const uint8_t* p, Words<2>) {
+  Words<2> r;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+  return r;
+}
+
+__device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e) {
+  if (e.n == 0) return 0;
+  return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.len + kCell - 1) / kCell);
+}
+
+template <int FMT, int DIM>
+__global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows(const RowsArgs a) {
+  constexpr int kChunks = DIM / 64;              // 16-byte pieces of a key in a thread
+  constexpr int kWide = DIM / 32;                // words of a value in a thread
+  constexpr int kTiles = DIM / 8;                // output tiles of eight dims
+  __shared__ int64_t sums[kWarps];
+  __shared__ int64_t found_lo;
+  __shared__ int found_b;
+  __shared__ float stat_m[kWarps][kRows], stat_l[kWarps][kRows];
+  extern __shared__ float joined[];              // [warps][16][DIM + 4]
+  pdl_prologue();
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
+
+  // ---- this thread block's share: all cells in one line, sequence by sequence, head by head, rows by rows
+  auto scan = [&](int base, int64_t& mine) {     // this thread's sequence's cells; the sum up to and with it
+    const int b = base + tid;
+    mine = b < c.batch ? cells_of(a, extent_of(c, b)) : 0;
+    int64_t up = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += t; }
+    if (lane == 31) sums[warp] = up;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) up += sums[w];
+    return up;
+  };
+  int64_t total = 0, mine;
+  for (int base = 0; base < c.batch; base += kWarps * 32) {
+    scan(base, mine);
+    for (int w = 0; w < kWarps; ++w) total += sums[w];
+    __syncthreads();
+  }
+  const int blocks = (int)min((int64_t)gridDim.x, (total + kWarps - 1) / kWarps);      // a cell for each warp at least
+  const int64_t lo = (int)blockIdx.x < blocks ? total * blockIdx.x / blocks : total;
+  const int64_t hi = (int)blockIdx.x < blocks ? total * (blockIdx.x + 1) / blocks : total;
+  if (lo >= hi) {
+    if (tid == 0) a.shares[blockIdx.x] = Share{total, total, total, 0, 0};
+    return;
+  }
+  int64_t before = 0;
+  for (int base = 0; base < c.batch; base += kWarps * 32) {
+    const int64_t up = scan(base, mine) + before;
+    if (up - mine <= lo && lo < up) { found_b = base + tid; found_lo = up - mine; }
+    for (int w = 0; w < kWarps; ++w) before += sums[w];
+    __syncthreads();
+    if (before > lo) break;
+  }
+  int b = found_b;
+  int64_t at = found_lo;                         // where sequence b's cells begin
+
+  // ---- its rows one after another
+  bool first = true;
+  for (int64_t pos = lo; pos < hi; ++b) {
+    const Extent e = extent_of(c, b);
+    const int64_t mine_all = cells_of(a, e);
+    if (mine_all == 0) continue;
+    const int per = max(1, (e.len + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
+    for (int item = (int)((pos - at) / per); pos < hi && item < c.kv_heads * tiles; ++item) {
+      const int64_t start = at + (int64_t)item * per, end = start + per;
+      if (first && tid == 0) a.shares[blockIdx.x] = Share{lo, start, end, b, item};
+      const int head = item / tiles, row0 = (item - head * tiles) * kRows;
+      const int rows = min(kRows, e.n * a.group - row0);
+      // keys up to the position of the row's token; a token whose position is below 0 sees none
+      auto limit_of = [&](int r) { return r < rows ? max(0, e.len - e.n + (row0 + r) / a.group + 1) : 0; };
+      const int limit[2] = {limit_of(g), limit_of(g + 8)};
+      const int least = limit_of(0), most = limit_of(rows - 1);
+      // (a 64-bit min(end, hi) in place of the choice was compiled to per in all but a share's first rows: nvcc 12.9)
+      const int cell0 = (int)(pos - start), quota = hi < end ? (int)(hi - start) : per, cell1 = min(quota, (most + kCell - 1) / kCell);
+
+      // ---- queries: rows g and g + 8, in the order of dims in which a thread has its part of a key
+      uint32_t q[4 * kChunks][4];
+      float factor[2];
+      {
+        const __nv_bfloat16* from[2];
+        float top[2] = {0.f, 0.f};
+        uint2 raw[2][4 * kChunks];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int row = row0 + g + 8 * r, token = row / a.group;
+          from[r] = a.q + (e.first + token) * a.ld_q + ((int64_t)head * a.group + row - token * a.group) * c.dim;
+#pragma unroll
+          for (int s = 0; s < 4 * kChunks; ++s) {
+            const int d = (cc + 4 * (s >> 2)) * 16 + 4 * (s & 3);
+            raw[r][s] = g + 8 * r < rows && d < c.dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0u, 0u);
+            top[r] = fmaxf(top[r], fmaxf(fmaxf(fabsf(bf16_lo(raw[r][s].x)), fabsf(bf16_hi(raw[r][s].x))),
+                                         fmaxf(fabsf(bf16_lo(raw[r][s].y)), fabsf(bf16_hi(raw[r][s].y)))));
+          }
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          // the power of two that brings the row's largest magnitude to 2^14 .. 2^15
+          const int ex = (int)(__float_as_uint(top[r]) >> 23) - 127;
+          const int up = top[r] == 0.f || ex == 128 ? 0 : min(14 - ex, 120);
+          const float by = __uint_as_float((uint32_t)(127 + max(up, -126)) << 23);
+          factor[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - max(up, -126)) << 23);
+#pragma unroll
+          for (int s = 0; s < 4 * kChunks; ++s) {
+            q[s][r] = pack_half2(bf16_lo(raw[r][s].x) * by, bf16_hi(raw[r][s].x) * by);
+            q[s][2 + r] = pack_half2(bf16_lo(raw[r][s].y) * by, bf16_hi(raw[r][s].y) * by);
+          }
+        }
+      }
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      float o[kTiles][4];
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
+
+      // ---- cells: keys and values of 32 tokens, the next cell's on their way
+      Words<4> k[4][kChunks];
+      Words<kWide> v[2][4];
+      float dk[2], dv[2];
+      auto pages = [&](int cell, int (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int token = cell * kCell + 16 * i;
+          p[i] = cell < cell1 && token < most ? page_of(c, b, token >> c.shift) : -1;
+        }
+      };
+      auto base_of = [&](int cell, int i, int page) {
+        const int token = cell * kCell + 16 * i;
+        return (((int64_t)page * c.kv_heads + head << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim;
+      };
+      auto load_k = [&](int cell, const int (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int64_t base = base_of(cell, i, p[i]);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int h = 0; h < kChunks; ++h) {
+              const int d = (cc + 4 * h) * 16;
+              k[2 * i + t][h] = p[i] >= 0 && d < c.dim ? load_words(c.k + base + (8 * t + g) * c.dim + d, Words<4>()) : Words<4>{};
+            }
+          // (a page that the table does not have, or has wrong: NaN for whoever sees its tokens)
+          dk[i] = p[i] >= 0 ? __ldg(c.dk + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+        }
+      };
+      auto load_v = [&](int cell, const int (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int64_t base = base_of(cell, i, p[i]);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int token = 2 * cc + (t & 1) + 8 * (t >> 1), d = g * 4 * kWide;
+            // (nothing of what lies behind the last key that is seen: its codes may be anything, and 0 times NaN is not 0)
+            v[i][t] = p[i] >= 0 && d < c.dim && cell * kCell + 16 * i + token < most ? load_words(c.v + base + token * c.dim + d, Words<kWide>())
+                                                                                    : Words<kWide>{};
+          }
+          dv[i] = p[i] >= 0 ? __ldg(c.dv + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+        }
+      };
+      int here[2], next[2];
+      int cell = cell0 + warp;
+      pages(cell, here);
+      if (cell < cell1) { load_k(cell, here); load_v(cell, here); }
+      pages(cell + kWarps, next);
+      for (; cell < cell1; cell += kWarps) {
+        // scores
+        float s[4][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
+#pragma unroll
+          for (int h = 0; h < kChunks; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t b0, b1;
+              half4_of<FMT>(k[t][h].w[j], b0, b1);
+              mma16(s[t], q[4 * h + j], b0, b1);
+            }
+        }
+        const float ck[2] = {dk[0], dk[1]}, cv[2] = {dv[0], dv[1]};
+        const bool more = cell + kWarps < cell1;
+        if (more) load_k(cell + kWarps, next);
+        // to the base 2, with the values' scales, masked
+        float top[2] = {m[0], m[1]};
+        float weigh[2], inverse[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool tiny = cv[i] < kLeastScale;
+          weigh[i] = tiny ? -60.f : lg2(cv[i]);
+          inverse[i] = tiny ? 1.1529215e18f : __frcp_rn(cv[i]);
+        }
+        const bool partial = (cell + 1) * kCell > least;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = i >> 1;
+            s[t][i] = fmaf(s[t][i], factor[r] * ck[t >> 1], weigh[t >> 1]);
+            if (partial && cell * kCell + 8 * t + 2 * cc + (i & 1) >= limit[r]) s[t][i] = -INFINITY;
+            top[r] = fmaxf(top[r], s[t][i]);
+          }
+        float from[2];
+        bool moved = false;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          moved |= top[r] > m[r];
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float shrink = m[r] == top[r] ? 1.f : ex2(m[r] - top[r]);
+            m[r] = top[r];
+            l[r] *= shrink;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) { o[t][2 * r] *= shrink; o[t][2 * r + 1] *= shrink; }
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) from[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
+        // weights, in the places of a left operand
+        uint32_t p[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float e0 = ex2(s[2 * i][2 * r] - from[r]), e1 = ex2(s[2 * i][2 * r + 1] - from[r]);
+            float e2 = ex2(s[2 * i + 1][2 * r] - from[r]), e3 = ex2(s[2 * i + 1][2 * r + 1] - from[r]);
+            const float sum = (e0 + e1) + (e2 + e3);
+            if (sum != 0.f) l[r] = fmaf(sum, inverse[i], l[r]);         // (nothing of a block that the row does not see, whatever its scale)
+            const bool none = cv[i] < kLeastScale;
+            p[i][r] = none ? 0u : pack_half2(e0, e1);
+            p[i][2 + r] = none ? 0u : pack_half2(e2, e3);
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int w = 0; w < kWide; ++w) {
+            uint32_t b[4][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x = v[i][2 * h].w[w], y = v[i][2 * h + 1].w[w];
+              half4_of<FMT>(__byte_perm(x, y, 0x5140), b[0][h], b[1][h]);
+              half4_of<FMT>(__byte_perm(x, y, 0x7362), b[2][h], b[3][h]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma16(o[4 * w + j], p[i], b[j][0], b[j][1]);
+          }
+        if (more) {
+          load_v(cell + kWarps, next);
+          pages(cell + 2 * kWarps, next);
+        }
+      }
+
+      // ---- the warps' sums together, and out
+      __syncthreads();                                                   // (the last rows' have been read)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        if (cc == 0) { stat_m[warp][g + 8 * r] = m[r]; stat_l[warp][g + 8 * r] = l[r]; }
+        if (g + 8 * r < rows) {
+          float* const to = joined + (warp * kRows + g + 8 * r) * (DIM + 4);
+          // tile t, column n stands for dim n * kTiles + t: a thread has columns 2 cc and 2 cc + 1
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < kTiles; t += 4)
+              *reinterpret_cast<float4*>(to + (2 * cc + h) * kTiles + t) =
+                  make_float4(o[t][2 * r + h], o[t + 1][2 * r + h], o[t + 2][2 * r + h], o[t + 3][2 * r + h]);
+        }
+      }
+      __syncthreads();
+      const bool whole = start >= lo && end <= hi;
+      const int slot = 2 * (int)blockIdx.x + (start < lo ? 0 : 1);
+      for (int i = tid; i < rows * (DIM / 4); i += kWarps * 32) {
+        const int r = i / (DIM / 4), d = i % (DIM / 4) * 4;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stat_m[w][r]);
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float by = stat_m[w][r] == top ? 1.f : ex2(stat_m[w][r] - top);
+          const float4 x = *reinterpret_cast<const float4*>(joined + (w * kRows + r) * (DIM + 4) + d);
+          sum = fmaf(stat_l[w][r], by, sum);
+          y.x = fmaf(x.x, by, y.x); y.y = fmaf(x.y, by, y.y); y.z = fmaf(x.z, by, y.z); y.w = fmaf(x.w, by, y.w);
+        }
+        if (whole) {
+          const int row = row0 + r, token = row / a.group, h = head * a.group + row - token * a.group;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          if (d < c.dim)
+            *reinterpret_cast<uint2*>(a.out + (e.first + token) * a.ld_out + (int64_t)h * c.dim + d) =
+                make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+          if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (top - 14.f)) * 0.69314718f;
+        } else {
+          float* const to = a.parts + ((int64_t)slot * kRows + r) * (DIM + 2);
+          to[d] = y.x; to[d + 1] = y.y; to[d + 2] = y.z; to[d + 3] = y.w;
+          if (d == 0) { to[DIM] = top; to[DIM + 1] = sum; }
+        }
+      }
+      first = false;
+      pos = min(end, hi);
+    }
+    at += mine_all;
+  }
+}
+
+// The rows whose keys several thread blocks have had, joined by the block whose share begins inside them first.  A row a thread block's quarter.
+template <int DIM>
+__global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid) {
+  pdl_prologue();
+  const int i = blockIdx.x + 1;
+  const Share s = a.shares[i];
+  if (s.lo <= s.start || s.lo >= s.end || a.shares[i - 1].lo > s.start) return;
+  const CacheView& c = a.c;
+  const Extent e = extent_of(c, s.b);
+  const int tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows), head = s.item / tiles, row0 = (s.item - head * tiles) * kRows;
+  const int rows = min(kRows, e.n * a.group - row0), d = threadIdx.x;
+  int last = i;
+  while (last + 1 < grid && a.shares[last + 1].lo < s.end) ++last;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    float top = -INFINITY, sum = 0.f, y = 0.f;
+    auto part = [&](int j) { return a.parts + ((int64_t)(2 * j + (j == i - 1 ? 1 : 0)) * kRows + r) * (DIM + 2); };
+    for (int j = i - 1; j <= last; ++j) top = fmaxf(top, part(j)[DIM]);
+#pragma unroll 4
+    for (int j = i - 1; j <= last; ++j) {
+      const float* const from = part(j);
+      const float by = from[DIM] == top ? 1.f : ex2(from[DIM] - top);
+      sum = fmaf(from[DIM + 1], by, sum);
+      y = fmaf(from[d], by, y);
+    }
+    const int row = row0 + r, token = row / a.group, h = head * a.group + row - token * a.group;
+    if (d < c.dim) a.out[(e.first + token) * a.ld_out + (int64_t)h * c.dim + d] = __float2bfloat16_rn(sum == 0.f ? 0.f : y / sum);
+    if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (top - 14.f)) * 0.69314718f;
+  }
+}
+
+constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + 255) / 256 * 256; }
+
+template <int FMT, int DIM>
+qm_status launch_rows(RowsArgs a, cudaStream_t s) {
+  constexpr auto kern = attention_rows<FMT, DIM>;
+  constexpr size_t smem = (size_t)kWarps * kRows * (DIM + 4) * 4;
+  static std::atomic<int> resident[kMaxDevices];
+  const int dev = current_device();
+  if (dev < 0) return QM_ERR_UNSUPPORTED;
+  int most = resident[dev].load(std::memory_order_relaxed);
+  if (most == 0) {
+    QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    QM_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&most, kern, kWarps * 32, smem));
+    most = std::min(kMaxBlocks, std::max(1, most) * sm_count());
+    resident[dev].store(most, std::memory_order_relaxed);
+  }
+  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)most), dim3(kWarps * 32), smem, s, a));
+  count_launch();
+  if (most > 1) {
+    QM_CUDA_OK(launch_pdl(attention_join<DIM>, dim3((unsigned)most - 1, 4), dim3(DIM), 0, s, a, most));
+    count_launch();
+  }
+  return QM_OK;
+}
+template <int FMT>
+qm_status launch_dim(const RowsArgs& a, cudaStream_t s) { return a.c.dim <= 64 ? launch_rows<FMT, 64>(a, s) : launch_rows<FMT, 128>(a, s); }
+
+}  // namespace
+
+size_t cache_attention_workspace(int dim) { return share_bytes() + (size_t)2 * kMaxBlocks * kRows * ((dim <= 64 ? 64 : 128) + 2) * 4; }
+
+qm_status launch_cache_attention(const CacheArgs& c, const AttentionArgs& l, cudaStream_t s) {
+  RowsArgs a{};
+  a.c = view_of(c);
+  a.q = static_cast<const __nv_bfloat16*>(l.q); a.ld_q = l.ld_q;
+  a.heads = l.heads; a.group = l.heads / c.kv_heads;
+  a.scale_log2 = l.scale * 1.44269504f;
+  a.out = static_cast<__nv_bfloat16*>(l.out); a.ld_out = l.ld_out; a.lse = l.lse;
+  a.shares = static_cast<Share*>(l.ws);
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(l.ws) + share_bytes());
+  return c.fmt == QM_FMT_INT8 ? launch_dim<QM_FMT_INT8>(a, s) : c.fmt == QM_FMT_E4M3 ? launch_dim<QM_FMT_E4M3>(a, s) : launch_dim<QM_FMT_E5M2>(a, s);
+}
+
+}  // namespace qm

@@ -1,0 +1,82 @@
+// What the cache's kernels share: its geometry, a sequence's extents with their checks, and 8-bit codes as pairs of fp16.  Included by .cu
+// files only; everything sits in the including file's anonymous namespace.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "quant_device.cuh"
+
+namespace qm {
+namespace {
+
+// Codes [blocks][kv_heads][block_tokens][dim], scales [blocks][kv_heads]; a sequence's blocks by its row of `tables`.
+struct CacheView {
+  uint8_t *k, *v;
+  float *dk, *dv;
+  int blocks, kv_heads, shift, dim;          // block_tokens is 1 << shift
+  const int32_t *tables, *lens, *starts;     // starts null: a new token for each sequence
+  int64_t ld_tables;
+  int table_width, batch;
+  int64_t tokens;
+};
+
+// A sequence's new tokens and its length with them.  What does not fit the tensors counts as no tokens at all.
+struct Extent { int64_t first; int n, len; };
+__device__ __forceinline__ Extent extent_of(const CacheView& c, int b) {
+  Extent e;
+  e.first = c.starts ? c.starts[b] : b;
+  const int64_t end = c.starts ? c.starts[b + 1] : b + 1;
+  e.n = e.first >= 0 && end >= e.first && end <= c.tokens ? (int)(end - e.first) : 0;
+  e.len = min(max(c.lens[b], 0), 0x7fff0000);       // (what is added to it stays inside 32 bits)
+  return e;
+}
+
+// The page that holds a sequence's block `i`; -1 where the table does not say or names none.
+__device__ __forceinline__ int page_of(const CacheView& c, int b, int i) {
+  if (i >= c.table_width) return -1;
+  const int p = __ldg(c.tables + (int64_t)b * c.ld_tables + i);
+  return p >= 0 && p < c.blocks ? p : -1;
+}
+
+// Two codes (the low 16 bits) as two fp16; all of them are on fp16's grid.
+template <int FMT>
+__device__ __forceinline__ uint32_t half2_of(uint32_t two) {
+  uint32_t h;
+  if (FMT == QM_FMT_E4M3) asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(h) : "r"(two));
+  else if (FMT == QM_FMT_E5M2) h = __byte_perm(two, 0u, 0x1404);                 // the upper half of an fp16
+  else {
+    // 1024 + (code + 128) is 0x6400 | (code ^ 0x80)
+    const uint32_t u = __byte_perm(two ^ 0x8080u, 0x64646464u, 0x4140);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(u), "r"(0x64806480u));
+  }
+  return h;
+}
+// Four codes as two pairs.
+template <int FMT>
+__device__ __forceinline__ void half4_of(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (FMT == QM_FMT_E4M3) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+  } else if (FMT == QM_FMT_E5M2) {
+    lo = __byte_perm(w, 0u, 0x1404);
+    hi = __byte_perm(w, 0u, 0x3424);
+  } else {
+    const uint32_t x = w ^ 0x80808080u;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(__byte_perm(x, 0x64646464u, 0x4140)), "r"(0x64806480u));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(__byte_perm(x, 0x64646464u, 0x4342)), "r"(0x64806480u));
+  }
+}
+
+inline CacheView view_of(const CacheArgs& a) {
+  CacheView c{};
+  c.k = a.k; c.v = a.v; c.dk = a.dk; c.dv = a.dv;
+  c.blocks = (int)a.blocks; c.kv_heads = a.kv_heads; c.dim = a.dim;
+  while ((1 << c.shift) < a.block_tokens) ++c.shift;
+  c.tables = a.tables; c.lens = a.lens; c.starts = a.starts;
+  c.ld_tables = a.ld_tables; c.table_width = a.table_width; c.batch = a.batch; c.tokens = a.tokens;
+  return c;
+}
+
+// Scales below this count as 0 (a magnitude of 5e-14 at most): the attention's sums weigh by their inverses.
+constexpr float kLeastScale = 8.6736174e-19f;                  // 2^-60
+
+}  // namespace
+}  // namespace qm

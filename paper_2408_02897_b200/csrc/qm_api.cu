@@ -483,6 +483,67 @@ qm_status qm_linear_fp8(const uint8_t* codes_x, int64_t ld_x, int32_t fmt_x, con
   return launch_linear_fp8(a, static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+qm_status to_cache(const qm_cache* c, int64_t tokens, CacheArgs* a) {
+  if (!c || tokens < 0 || c->batch < 0 || !valid_fmt(c->fmt)) return QM_ERR_INVALID_ARG;
+  if (c->blocks <= 0 || c->kv_heads <= 0 || c->block_tokens <= 0 || c->head_dim <= 0 || c->table_width <= 0) return QM_ERR_INVALID_ARG;
+  if (!c->starts && tokens != c->batch) return QM_ERR_INVALID_ARG;
+  if (c->block_tokens < 16 || c->block_tokens > 256 || (c->block_tokens & (c->block_tokens - 1)) || c->head_dim % 16 || c->head_dim > 128)
+    return QM_ERR_UNSUPPORTED;
+  if (tokens == 0 || c->batch == 0) return QM_OK;
+  if (!c->k_codes || !c->v_codes || !c->k_delta || !c->v_delta || !c->tables || !c->lens) return QM_ERR_INVALID_ARG;
+  if (c->batch > 1 && c->ld_tables < c->table_width) return QM_ERR_INVALID_ARG;
+  if (!sane(c->blocks) || !sane(tokens) || !sane(c->batch) || !sane_pitch(c->ld_tables) || c->kv_heads > 65536 ||
+      (int64_t)c->table_width * c->block_tokens > (1ll << 31) - 65536)
+    return QM_ERR_UNSUPPORTED;
+  if (addr(c->k_codes) % 16 || addr(c->v_codes) % 16 || addr(c->k_delta) % 4 || addr(c->v_delta) % 4 || addr(c->tables) % 4 || addr(c->lens) % 4 ||
+      addr(c->starts) % 4)
+    return QM_ERR_ALIGNMENT;
+  *a = CacheArgs{c->k_codes, c->v_codes, c->k_delta, c->v_delta, c->blocks, c->kv_heads, c->block_tokens, c->head_dim, c->fmt,
+                 c->tables, c->lens, c->starts, c->batch > 1 ? c->ld_tables : 0, c->table_width, c->batch, tokens};
+  return QM_OK;
+}
+// [tokens] rows of `row` elements, ld apart, 16-byte aligned
+qm_status check_rows(const void* p, int64_t tokens, int64_t* ld, int64_t row) {
+  if (!p || (tokens > 1 && *ld < row)) return QM_ERR_INVALID_ARG;
+  if (tokens == 1) *ld = row;
+  if (!sane_pitch(*ld) || row >= (1ll << 30)) return QM_ERR_UNSUPPORTED;
+  return addr(p) % 16 || *ld % 8 ? QM_ERR_ALIGNMENT : QM_OK;
+}
+}  // namespace
+
+qm_status qm_cache_append(const qm_cache* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int32_t dtype, int64_t tokens,
+                          void* stream) {
+  CacheArgs c{};
+  qm_status st = to_cache(cache, tokens, &c);
+  if (st != QM_OK) return st;
+  if (!valid_dtype(dtype)) return QM_ERR_INVALID_ARG;
+  if (c.tokens == 0) return QM_OK;
+  const int64_t row = (int64_t)c.kv_heads * c.dim;
+  if ((st = check_rows(k, tokens, &ld_k, row)) != QM_OK || (st = check_rows(v, tokens, &ld_v, row)) != QM_OK) return st;
+  return launch_cache_append(c, k, ld_k, v, ld_v, dtype, static_cast<cudaStream_t>(stream));
+}
+
+size_t qm_cache_attention_workspace_bytes(int32_t head_dim) {
+  return head_dim <= 0 || head_dim > 128 || head_dim % 16 ? 0 : cache_attention_workspace(head_dim);
+}
+
+qm_status qm_cache_attention(const qm_cache* cache, const void* q, int64_t ld_q, int32_t heads, float scale, int64_t tokens, void* out,
+                             int64_t ld_out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  CacheArgs c{};
+  qm_status st = to_cache(cache, tokens, &c);
+  if (st != QM_OK) return st;
+  if (heads <= 0 || heads % cache->kv_heads || !(scale >= -3.402823466e38f && scale <= 3.402823466e38f)) return QM_ERR_INVALID_ARG;
+  if (c.tokens == 0) return QM_OK;
+  const int64_t row = (int64_t)heads * c.dim;
+  if ((st = check_rows(q, tokens, &ld_q, row)) != QM_OK || (st = check_rows(out, tokens, &ld_out, row)) != QM_OK) return st;
+  if (!ws) return QM_ERR_INVALID_ARG;
+  if (!sane(tokens * (heads / c.kv_heads))) return QM_ERR_UNSUPPORTED;          // query rows of a cached head
+  if (addr(ws) % 256 || addr(lse) % 4) return QM_ERR_ALIGNMENT;
+  if (ws_bytes < cache_attention_workspace(c.dim)) return QM_ERR_WORKSPACE_TOO_SMALL;
+  return launch_cache_attention(c, {q, ld_q, heads, scale, out, ld_out, lse, ws}, static_cast<cudaStream_t>(stream));
+}
+
 size_t qm_metric_workspace_bytes(int64_t count) {
   if (count <= 0) return 0;
   return align256(sizeof(double) * kPartialDoubles * (size_t)metric_blocks(count));

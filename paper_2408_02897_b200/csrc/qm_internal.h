@@ -181,6 +181,26 @@ struct LinearFp8Args {
 };
 qm_status launch_linear_fp8(const LinearFp8Args& a, cudaStream_t s);
 
+// ---- cache of keys and values in 8 bits (cache_append.cu, cache_attention.cu) ----
+struct CacheArgs {
+  uint8_t *k, *v; float *dk, *dv;             // codes [blocks][kv_heads][block_tokens][dim], scales [blocks][kv_heads]
+  int64_t blocks; int kv_heads, block_tokens, dim, fmt;
+  const int32_t *tables, *lens, *starts;      // [batch][ld_tables], [batch], [batch + 1] or null
+  int64_t ld_tables; int table_width, batch;
+  int64_t tokens;
+};
+// k, v: [tokens][kv_heads][dim], ld_* elements between tokens
+qm_status launch_cache_append(const CacheArgs& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, cudaStream_t s);
+struct AttentionArgs {
+  const void* q; int64_t ld_q; int heads;     // bf16 [tokens][heads][dim]
+  float scale;
+  void* out; int64_t ld_out;                  // bf16
+  float* lse;                                 // [tokens][heads] or null
+  void* ws;                                   // cache_attention_workspace bytes
+};
+size_t cache_attention_workspace(int dim);
+qm_status launch_cache_attention(const CacheArgs& c, const AttentionArgs& a, cudaStream_t s);
+
 // ---- metric (metric.cu) ----------------------------------------------------
 // One partial record per CTA: {sum_be, max_be, sum_diff2, sum_ref2, sum_den2} as doubles.
 constexpr int kPartialDoubles = 5;
