@@ -20,76 +20,147 @@ struct BlockArgs {
 };
 
 // A block's scale from the bits of its maximum.  One that holds a NaN or Inf gets NaN and codes 0; one so small that the quotient with
-// qmax is 0 in fp32 counts as one of zeros.
-struct BlockScale {
-  float delta;
-  bool pair, zero;             // whether the two-wide quotient serves, and whether the codes are all 0
-};
+// qmax is 0 in fp32 counts as one of zeros.  `recip` is 0 where the two-wide quotient does not serve or the codes are all 0.
+struct BlockScale { float delta, recip; };
 template <int FMT>
 __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
   BlockScale s;
-  const float d = __fdiv_rn(__uint_as_float(top), fmt_qmax(FMT));
-  s.zero = top >= 0x7f800000u || (top != 0 && d == 0.f);
-  s.delta = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : d == 0.f ? 1.f : d;
-  s.pair = QuotientPair::serves(s.delta);
+  const float x = __uint_as_float(top), qmax = fmt_qmax(FMT);
+  if (top >= 0x26800000u && top < 0x58800000u) {                // 2^-50 .. 2^50: the division by two corrections (see Quotient)
+    constexpr float r = FMT == QM_FMT_E4M3 ? 1.f / 448.f : 1.f / 57344.f;
+    const float q0 = x * r, q1 = fmaf(fmaf(-q0, qmax, x), r, q0);
+    s.delta = fmaf(fmaf(-q1, qmax, x), r, q1);
+    s.recip = __frcp_rn(s.delta);
+  } else {
+    const float d = __fdiv_rn(x, qmax);
+    s.delta = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : d == 0.f ? 1.f : d;
+    s.recip = QuotientPair::serves(s.delta) && (top == 0 || d != 0.f) ? __frcp_rn(s.delta) : 0.f;
+  }
   return s;
 }
-// under scales outside QuotientPair's range
+// Two codes under a scale that the two-wide quotient does not serve, or of a block whose codes are all 0 (delta is 1 or NaN then).
 template <int FMT>
 __device__ __noinline__ uint32_t far_pair(float x0, float x1, float delta) {
+  if (!(delta < INFINITY) || QuotientPair::serves(delta)) return 0u;
   const Quotient quot(delta);
-  return quant2<FMT>(quot(x0), quot(x1));
+  return quant2<FMT>(quot(x0), quot(x1)) & 0xffffu;
+}
+__device__ __forceinline__ QuotientPair quotient_of(const BlockScale& s) {
+  uint64_t r, d;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(s.recip));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(-s.delta));
+  return QuotientPair(r, d);
 }
 template <int FMT>
-__device__ __forceinline__ uint32_t codes2(float x0, float x1, const BlockScale& s, const QuotientPair& quot) {
-  if (s.pair) return s.zero ? 0u : quant_pair_x2<FMT>(x0, x1, quot);
-  return s.zero ? 0u : far_pair<FMT>(x0, x1, s.delta) & 0xffffu;
+__device__ __forceinline__ uint32_t cvt_pair(uint64_t q) {
+  float lo, hi;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(q));
+  return quant2<FMT>(lo, hi);
 }
-template <int FMT>
-__device__ __forceinline__ uint2 codes8(const Vec8& v, const BlockScale& s, const QuotientPair& quot) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = codes2<FMT>(v.v[2 * i], v.v[2 * i + 1], s, quot);
-  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-}
-
-// Elements c .. c + 8 of a row, zeros from `cols` on.
-template <typename T>
-__device__ __forceinline__ Vec8 row8(const T* row, int c, int cols) {
-  if (c + 8 <= cols) return Loader<T>::load8(row + c);
-  Vec8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v.v[i] = c + i < cols ? Loader<T>::load1(row, c + i) : 0.f;
+__device__ __forceinline__ uint64_t pair_of_bits(uint32_t lo, uint32_t hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
   return v;
 }
 
-// 32 rows x 512 contraction entries a thread block.
+// Eight consecutive elements of a row as they lie in memory, zeros beyond its end.
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+  uint4 q;
+  __device__ __forceinline__ uint32_t top() const {               // as fp32's bits
+    constexpr uint32_t k = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vmaxu2(q.x & k, q.y & k), __vmaxu2(q.z & k, q.w & k));
+    return max(m << 16, m & 0xffff0000u);
+  }
+  // the quotient of a zero loses its sign: all signs are put back, four at a time
+  template <int FMT>
+  static __device__ __forceinline__ uint32_t codes4(uint32_t a, uint32_t b, const QuotientPair& quot) {
+    const uint32_t lo = cvt_pair<FMT>(quot(pair_of_bits(a << 16, a & 0xffff0000u))), hi = cvt_pair<FMT>(quot(pair_of_bits(b << 16, b & 0xffff0000u)));
+    return __byte_perm(lo, hi, 0x5410) | (__byte_perm(a, b, 0x7531) & 0x80808080u);
+  }
+  template <int FMT>
+  __device__ __forceinline__ uint2 codes(const BlockScale& s) const {
+    if (s.recip != 0.f) {
+      const QuotientPair quot = quotient_of(s);
+      return make_uint2(codes4<FMT>(q.x, q.y, quot), codes4<FMT>(q.z, q.w, quot));
+    }
+    auto two = [&](uint32_t w) { return far_pair<FMT>(bf16_lo(w), bf16_hi(w), s.delta); };
+    return make_uint2(two(q.x) | two(q.y) << 16, two(q.z) | two(q.w) << 16);
+  }
+  static __device__ __forceinline__ Eight load(const __nv_bfloat16* row, int c, int cols) {
+    Eight v;
+    if (c + 8 <= cols) {
+      v.q = __ldg(reinterpret_cast<const uint4*>(row + c));
+      return v;
+    }
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + i) : 0u;
+    v.q = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    return v;
+  }
+};
+template <> struct Eight<float> {
+  Vec8 v;
+  __device__ __forceinline__ uint32_t top() const { return absmax8(v, 0u); }
+  template <int FMT>
+  __device__ __forceinline__ uint2 codes(const BlockScale& s) const {
+    uint32_t w[4];
+    if (s.recip != 0.f) {
+      const QuotientPair quot = quotient_of(s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = quant_pair_x2<FMT>(v.v[2 * i], v.v[2 * i + 1], quot);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = far_pair<FMT>(v.v[2 * i], v.v[2 * i + 1], s.delta);
+    }
+    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+  }
+  static __device__ __forceinline__ Eight load(const float* row, int c, int cols) {
+    Eight e;
+    if (c + 8 <= cols) {
+      e.v = Loader<float>::load8(row + c);
+      return e;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.v.v[i] = c + i < cols ? __ldg(row + c + i) : 0.f;
+    return e;
+  }
+};
+
+// 32 rows x 512 contraction entries a thread block, eight lanes to a row's block of 128, four blocks of the row each.  What a block costs once (its
+// scale and the reciprocal) is computed for all four at a time, one in two of the eight lanes.
 template <typename T, int FMT>
-__global__ void __launch_bounds__(kThreads) blocks_rows(const BlockArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) blocks_rows(const BlockArgs a) {
   pdl_prologue();
   const int j = threadIdx.x & 7, kb0 = blockIdx.y * 4;
   const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
   const bool in = row < a.nc;
   const T* const x = static_cast<const T*>(a.x) + (in ? row : 0) * a.ld;
-  Vec8 v[4][2];
+  Eight<T> v[4][2];
+  uint32_t m[4];
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) v[b][h] = row8(x, (kb0 + b) * kScaleBlock + 64 * h + 8 * j, a.c);
+    for (int h = 0; h < 2; ++h) v[b][h] = Eight<T>::load(x, (kb0 + b) * kScaleBlock + 64 * h + 8 * j, a.c);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) m[b] = max(v[b][0].top(), v[b][1].top());
+  // the maxima of the eight lanes: lane j ends with that of block j / 2
+  const bool b2 = j & 4, b1 = j & 2;
+  uint32_t m0 = max(b2 ? m[2] : m[0], __shfl_xor_sync(0xffffffffu, b2 ? m[0] : m[2], 4));
+  uint32_t m1 = max(b2 ? m[3] : m[1], __shfl_xor_sync(0xffffffffu, b2 ? m[1] : m[3], 4));
+  m0 = max(b1 ? m1 : m0, __shfl_xor_sync(0xffffffffu, b1 ? m0 : m1, 2));
+  m0 = max(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
+  const BlockScale mine = block_scale<FMT>(m0);
+  if ((j & 1) == 0 && in && (kb0 + (j >> 1)) * kScaleBlock < a.c) a.delta[(int64_t)(kb0 + (j >> 1)) * a.delta_cols + row] = mine.delta;
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
-    uint32_t top = absmax8(v[b][1], absmax8(v[b][0], 0u));
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const BlockScale s = block_scale<FMT>(top);
-    const QuotientPair quot(s.delta);
-    const int k0 = (kb0 + b) * kScaleBlock;
-    if (!in || k0 >= a.c) continue;
-    if (j == 0) a.delta[(int64_t)(kb0 + b) * a.delta_cols + row] = s.delta;
+    const int from = (threadIdx.x & 24) + 2 * b;
+    const BlockScale s{__shfl_sync(0xffffffffu, mine.delta, from), __shfl_sync(0xffffffffu, mine.recip, from)};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = k0 + 64 * h + 8 * j;
-      if (c < a.ldc) *reinterpret_cast<uint2*>(a.codes + row * a.ldc + c) = codes8<FMT>(v[b][h], s, quot);
+      const int c = (kb0 + b) * kScaleBlock + 64 * h + 8 * j;
+      if (in && c < a.ldc) *reinterpret_cast<uint2*>(a.codes + row * a.ldc + c) = v[b][h].template codes<FMT>(s);
     }
   }
 }
@@ -100,26 +171,25 @@ __global__ void __launch_bounds__(kThreads) blocks_squares(const BlockArgs a) {
   pdl_prologue();
   const int c = blockIdx.x * kScaleBlock + 8 * (threadIdx.x & 15);
   const int64_t row0 = (int64_t)blockIdx.y * 128 + (threadIdx.x >> 4);
-  Vec8 v[8];
+  Eight<T> v[8];
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = row0 + 16 * i;
-    v[i] = row8(static_cast<const T*>(a.x) + (row < a.nc ? row : 0) * a.ld, c, row < a.nc ? a.c : 0);
-    top = absmax8(v[i], top);
+    v[i] = Eight<T>::load(static_cast<const T*>(a.x) + (row < a.nc ? row : 0) * a.ld, c, row < a.nc ? a.c : 0);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, v[i].top());
   __shared__ uint32_t tops[kThreads / 32];
   top = __reduce_max_sync(0xffffffffu, top);
   if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
   __syncthreads();
-  top = __reduce_max_sync(0xffffffffu, tops[threadIdx.x & 7]);
-  const BlockScale s = block_scale<FMT>(top);
-  const QuotientPair quot(s.delta);
+  const BlockScale s = block_scale<FMT>(__reduce_max_sync(0xffffffffu, tops[threadIdx.x & 7]));
   if (threadIdx.x == 0) a.delta[(int64_t)blockIdx.x * a.delta_cols + blockIdx.y] = s.delta;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = row0 + 16 * i;
-    if (row < a.nc && c < a.ldc) *reinterpret_cast<uint2*>(a.codes + row * a.ldc + c) = codes8<FMT>(v[i], s, quot);
+    if (row < a.nc && c < a.ldc) *reinterpret_cast<uint2*>(a.codes + row * a.ldc + c) = v[i].template codes<FMT>(s);
   }
 }
 
@@ -178,7 +248,7 @@ __global__ void __launch_bounds__(kThreads) blocks_strided(const BlockArgs a) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const BlockScale s = block_scale<FMT>(top[h]);
-    const QuotientPair quot(s.delta);
+    const QuotientPair quot = quotient_of(s);
     if (SUB == 1) {
       const int64_t r = r0 + 2 * lane + h;
       if (w == 0 && r < a.nc) a.delta[(int64_t)blockIdx.y * a.delta_cols + r] = s.delta;
@@ -189,7 +259,8 @@ __global__ void __launch_bounds__(kThreads) blocks_strided(const BlockArgs a) {
     for (int u = 0; u < SUB; ++u) {
       uint32_t c[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = codes2<FMT>(v[u][2 * i][h], v[u][2 * i + 1][h], s, quot);
+      for (int i = 0; i < 8; ++i) c[i] = s.recip != 0.f ? quant_pair_x2<FMT>(v[u][2 * i][h], v[u][2 * i + 1][h], quot)
+                                                             : far_pair<FMT>(v[u][2 * i][h], v[u][2 * i + 1][h], s.delta);
       *reinterpret_cast<uint4*>(&turned[64 * u + 2 * lane + h][16 * w]) =
           make_uint4(c[0] | c[1] << 16, c[2] | c[3] << 16, c[4] | c[5] << 16, c[6] | c[7] << 16);
     }
