@@ -23,6 +23,23 @@ __device__ __forceinline__ float load_bias(const BlockScales& s, int64_t n) {
   if (!s.bias) return 0.f;
   return s.bias_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(s.bias)[n]) : static_cast<const float*>(s.bias)[n];
 }
+// acc += scale * (two sums out of tensor memory). Volatile, so that it stays behind the wait for them.
+__device__ __forceinline__ void add_scaled(uint64_t& acc, uint32_t lo, uint32_t hi, uint64_t scale) {
+  asm volatile("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(acc) : "r"(lo), "r"(hi), "l"(scale));
+}
+__device__ __forceinline__ void add_scaled(uint64_t& acc, uint32_t lo, uint32_t hi, uint64_t column, uint64_t scale) {
+  asm volatile("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tmul.rn.f32x2 v, v, %3;\n\tfma.rn.f32x2 %0, v, %4, %0;\n\t}"
+               : "+l"(acc) : "r"(lo), "r"(hi), "l"(column), "l"(scale));
+}
+// Scales on their way to shared memory, four bytes a copy (0 where there is none): a block's are asked for several blocks ahead, which registers
+// that are handed on from round to round would wait for a round later.
+__device__ __forceinline__ void copy4(uint32_t dst, const float* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4u : 0u) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+constexpr int kAhead = 6;                      // blocks whose scales are in shared memory or on their way there
+
 __device__ __forceinline__ void add4(float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
 
 // ------------------------------------------------------------------ few rows
@@ -45,10 +62,10 @@ constexpr int kFewStages = 12;
 constexpr int kMaxSplit = 8;
 __host__ __device__ constexpr int few_cols(int nt) { return nt < 32 ? nt : nt / 2; }            // columns of a thread
 __host__ __device__ constexpr int few_bufs(int nt) { return nt < 128 ? 4 : 2; }                 // blocks' sums in tensor memory
+__host__ __device__ constexpr uint32_t few_scale_bytes(int nt) { return kEpiWarps * kAhead * (few_cols(nt) + 32) * 4; }
 struct SharedFew {
   uint64_t full[kFewStages], empty[kFewStages], sum_full[4], sum_empty[4], drain, read;
   uint32_t tmem_base, abort_flag, gave_up, pad;        // gave_up: some CTA of the cluster did
-  alignas(16) float dx[kEpiWarps][2][64];
 };
 
 template <typename T, int NT>
@@ -60,7 +77,9 @@ linear_fp8_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
   constexpr uint32_t kStage = kBlockBytes + (uint32_t)NT * kBlock, kTmemCols = NT * kBufs;
   // behind the ring: of a split contraction the parts' sums of this CTA's rows, [part][row][weight row]
   float* const sums = reinterpret_cast<float*>(tiles + (size_t)a.stages * kStage);
-  SharedFew* sh = reinterpret_cast<SharedFew*>(reinterpret_cast<uint8_t*>(sums) + a.sums_bytes);
+  // (16-byte aligned, as everything here)
+  float* const scales = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(sums) + a.sums_bytes);
+  SharedFew* sh = reinterpret_cast<SharedFew*>(reinterpret_cast<uint8_t*>(scales) + few_scale_bytes(NT));
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int tile = (int)blockIdx.x / a.split, part = (int)blockIdx.x - tile * a.split;
   const int n0 = tile / a.tiles_m * kBlock, m0 = tile % a.tiles_m * NT;
@@ -170,46 +189,48 @@ linear_fp8_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     if (NT >= 32 || h == 0) {
       const int64_t n = (int64_t)n0 + q * 32 + lane;
       const int64_t wcol = a.sc.side == 1 ? (n < a.N ? n : a.N - 1) : n0 / kBlock;
-      // scales are fetched two blocks ahead, those of x a column a lane
-      auto fetch_w = [&](int kb) { return kb < kb1 ? a.sc.dw[(int64_t)kb * a.sc.dw_cols + wcol] : 0.f; };
-      auto fetch_x = [&](int kb, int c) { return kb < kb1 && c < live ? a.sc.dx[(int64_t)kb * a.M + m0 + c] : 0.f; };
-      constexpr int kPer = kCols > 32 ? 2 : 1;
-      float nw[2], nx[2][kPer];
+      // a block's scales: of x for the thread's columns, then of the weights for the warp's 32 lanes (or one for all)
+      constexpr int kSlot = kCols + 32;
+      float* const ring = scales + (warp - 2) * kAhead * kSlot;
+      auto fetch = [&](int kb, int slot) {
+        if (kb < kb1) {
+          const uint32_t to = smem_u32(ring + slot * kSlot + lane);
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        nw[d] = fetch_w(kb0 + d);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) nx[d][i] = fetch_x(kb0 + d, c0 + 32 * i + lane);
-      }
+          for (int i = 0; i < kCols; i += 32)
+            if (kCols >= 32 || lane < kCols) {
+              const bool there = c0 + i + lane < live;
+              copy4(to + i * 4, a.sc.dx + (int64_t)kb * a.M + (there ? m0 + c0 + i + lane : m0), there);
+            }
+          copy4(to + kCols * 4, a.sc.dw + (int64_t)kb * a.sc.dw_cols + wcol, true);
+        }
+        copies_commit();
+      };
+      for (int d = 0; d < kAhead - 1; ++d) fetch(kb0 + d, d);
       const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16) + c0;
+      int slot = 0;
       for (int kb = kb0, g = 0; kb < kb1; ++kb, ++g) {
         const int buf = g % kBufs;
-        float* const dx = sh->dx[warp - 2][g & 1];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (kCols >= 32 || lane < kCols) dx[32 * i + lane] = nx[0][i];
-        const uint64_t dw = both(nw[0]);
-        nw[0] = nw[1];
-        nw[1] = fetch_w(kb + 2);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) { nx[0][i] = nx[1][i]; nx[1][i] = fetch_x(kb + 2, c0 + 32 * i + lane); }
-        ok = w.wait_warp(smem_u32(&sh->sum_full[buf]), (uint32_t)(g / kBufs) & 1u);      // (and the scales are in shared memory)
-        __syncwarp();
+        copies_wait<kAhead - 2>();
+        __syncwarp();                                                        // (and the slot that is filled next has been read by all lanes)
+        fetch(kb + kAhead - 1, slot == 0 ? kAhead - 1 : slot - 1);
+        const float* const dx = ring + slot * kSlot;
+        const uint64_t dw = both(dx[kCols + lane]);
+        slot = slot == kAhead - 1 ? 0 : slot + 1;
+        ok = w.wait_warp(smem_u32(&sh->sum_full[buf]), (uint32_t)(g / kBufs) & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int c = 0; c < kCols; c += 16) {
           uint32_t r[16];
           tmem_ld16(lane_addr + buf * NT + c, r);
-          tmem_ld_wait();
-          landed(r);
+          float4 d[4];
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const float4 d = *reinterpret_cast<const float4*>(dx + c + i);
-            uint64_t& lo = acc[(c + i) / 2];
-            uint64_t& hi = acc[(c + i) / 2 + 1];
-            lo = fma2(mul2(pair_of(d.x, d.y), dw), pair_of(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), lo);
-            hi = fma2(mul2(pair_of(d.z, d.w), dw), pair_of(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), hi);
+          for (int i = 0; i < 4; ++i) d[i] = *reinterpret_cast<const float4*>(dx + c + 4 * i);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            add_scaled(acc[c / 2 + 2 * i], r[4 * i], r[4 * i + 1], mul2(pair_of(d[i].x, d[i].y), dw));
+            add_scaled(acc[c / 2 + 2 * i + 1], r[4 * i + 2], r[4 * i + 3], mul2(pair_of(d[i].z, d[i].w), dw));
           }
         }
         tc_fence_before();
@@ -217,6 +238,7 @@ linear_fp8_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         if (lane == 0) mbar_arrive(smem_u32(&sh->sum_empty[buf]));
       }
     }
+    copies_wait<0>();                                                         // (of scales that a kernel which gives up has not used)
     if (lane == 0) mbar_arrive(smem_u32(&sh->read));
     if (a.split == 1) {
       const int64_t n = (int64_t)n0 + q * 32 + lane;
@@ -294,10 +316,13 @@ template <int N> __device__ __forceinline__ void regs_down() { asm volatile("set
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 constexpr uint32_t kManyStageBytes = 2 * kBlockBytes;
 constexpr uint32_t kOutBytes = 32 * 128;       // of output on its way per epilogue warp: 32 rows of 128 bytes
+// floats of a block's scales in a warp's ring: 32 rows, and 128 columns or one
+__host__ __device__ constexpr int many_slot(bool side1) { return side1 ? 160 : 36; }
+__host__ __device__ constexpr uint32_t many_scale_bytes(bool side1) { return kEpiWarps * kAhead * many_slot(side1) * 4; }
 struct SharedMany {
   uint64_t full[kManyStages], empty[kManyStages], sum_full[2], sum_empty[2], drain;
   uint32_t tmem_base, abort_flag, issued, peer_gave_up, peer_issued, pad[3];
-  alignas(16) float dw[2][256], bias[256];
+  alignas(16) float bias[256];
 };
 
 // 32 (fp32) or 64 (bf16) columns of a thread's row to the warp's staging buffer: rows of 128 bytes, 16-byte units permuted with the row.
@@ -329,7 +354,8 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* const staging = tiles + (size_t)kManyStages * kManyStageBytes;
-  SharedMany* sh = reinterpret_cast<SharedMany*>(staging + kEpiWarps * kOutBytes);
+  float* const scales = reinterpret_cast<float*>(staging + kEpiWarps * kOutBytes);
+  SharedMany* sh = reinterpret_cast<SharedMany*>(reinterpret_cast<uint8_t*>(scales) + many_scale_bytes(SIDE1));
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
@@ -396,11 +422,11 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       for (int t = pair; t < a.num_tiles && ok; t += num_pairs) {
         for (int kb = 0; kb < a.num_kb; ++kb, ++it) {
           const uint32_t buf = it & 1;
-          if (it >= 2 && !w.wait_warp(smem_u32(&sh->sum_empty[buf]), ((it >> 1) - 1) & 1)) { ok = false; break; }
           if (!w.wait_warp(smem_u32(&sh->full[s]), parity)) { ok = false; break; }
-          tc_fence_after();
           const uint32_t base = smem_u32(tiles) + (uint32_t)s * kManyStageBytes;
           const uint64_t da = smem_desc(base, 128), db = smem_desc(base + kBlockBytes, 128);
+          if (it >= 2 && !w.wait_warp(smem_u32(&sh->sum_empty[buf]), ((it >> 1) - 1) & 1)) { ok = false; break; }
+          tc_fence_after();
           if (lead) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) mma_pair<kKindF8>(tmem_base + buf * 256, da + 2 * k, db + 2 * k, a.idesc, k ? 1u : 0u, true);
@@ -423,25 +449,38 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const bool has_bias = a.sc.bias != nullptr;
     bool ok = true;
     uint32_t it = 0;
-    // Scales are fetched two blocks ahead of their use, across the ends of tiles.
-    int ft = pair, fkb = 0;
-    int64_t frow = 0, fcol = 0;
-    auto place = [&]() {
-      const int tm = ft / a.tiles_n;
-      frow = (int64_t)tm * 256 + rank * kBlock + q * 32 + lane;
-      const int64_t c = (int64_t)(ft - tm * a.tiles_n) * 256;
-      fcol = SIDE1 ? c + et : c / kBlock + h;
+    // A block's scales: of x for the warp's 32 rows, then of the weight for its 128 columns.  They are asked for across the ends of tiles.
+    constexpr int kSlot = many_slot(SIDE1);
+    float* const ring = scales + (warp - 4) * kAhead * kSlot;
+    int ft = pair, left = 0, put = 0, slot = 0, in_w = 0;
+    const float *px = nullptr, *pw = nullptr;
+    bool in_x = false;
+    auto fetch = [&]() {
+      if (left == 0 && ft < a.num_tiles) {
+        const int tm = ft / a.tiles_n;
+        const int64_t row = (int64_t)tm * 256 + rank * kBlock + q * 32 + lane, c = (int64_t)(ft - tm * a.tiles_n) * 256 + h * 128;
+        const int64_t col = SIDE1 ? c + lane : c / kBlock;
+        in_x = row < a.M;
+        in_w = col < a.sc.dw_cols ? (int)(a.sc.dw_cols - col < 128 ? a.sc.dw_cols - col : 128) : 0;         // columns from this lane's on
+        px = a.sc.dx + (in_x ? row : 0); pw = a.sc.dw + (in_w ? col : 0);
+        left = a.num_kb;
+      }
+      if (left > 0) {
+        const uint32_t to = smem_u32(ring + put * kSlot + lane);
+        copy4(to, px, in_x);
+        if (SIDE1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) copy4(to + 128 * (i + 1), in_w > 32 * i ? pw + 32 * i : a.sc.dw, in_w > 32 * i);
+        } else if (lane == 0) {
+          copy4(to + 128, pw, in_w > 0);
+        }
+        px += a.M; pw += a.sc.dw_cols;
+        if (--left == 0) ft += num_pairs;
+      }
+      copies_commit();
+      put = put == kAhead - 1 ? 0 : put + 1;
     };
-    place();
-    auto fetch = [&](float& x, float& dw) {
-      const bool in = ft < a.num_tiles;
-      x = in && frow < a.M ? a.sc.dx[(int64_t)fkb * a.M + frow] : 0.f;
-      dw = in && fcol < a.sc.dw_cols ? a.sc.dw[(int64_t)fkb * a.sc.dw_cols + fcol] : 0.f;
-      if (++fkb == a.num_kb) { fkb = 0; ft += num_pairs; place(); }
-    };
-    float x0, x1, w0, w1;
-    fetch(x0, w0);
-    fetch(x1, w1);
+    for (int d = 0; d < kAhead - 1; ++d) fetch();
     for (int t = pair; t < a.num_tiles; t += num_pairs) {
       const int tm = t / a.tiles_n;
       const int64_t c0 = (int64_t)(t - tm * a.tiles_n) * 256;
@@ -456,36 +495,41 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
       for (int kb = 0; kb < a.num_kb; ++kb, ++it) {
-        const uint32_t buf = it & 1;
-        const uint64_t scale = both(SIDE1 ? x0 : x0 * w0);
-        if (SIDE1) {
-          sh->dw[buf][et] = w0;
-          asm volatile("bar.sync 1, 256;" ::: "memory");                      // (whoever is here has read the block before)
-        }
-        x0 = x1; w0 = w1;
-        fetch(x1, w1);
+        const uint32_t buf = it & 1, from = tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256 + h * 128;
+        copies_wait<kAhead - 2>();
+        __syncwarp();                                                         // (and the slot that is filled next has been read by all lanes)
+        fetch();
+        const float* const sc = ring + slot * kSlot;
+        const uint64_t scale = both(SIDE1 ? sc[lane] : sc[lane] * sc[32]);
+        slot = slot == kAhead - 1 ? 0 : slot + 1;
+        float4 d[2][SIDE1 ? 4 : 1];
+        auto columns = [&](int c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[c & 1][SIDE1 ? i : 0] = *reinterpret_cast<const float4*>(sc + 32 + 16 * c + 4 * i);
+        };
+        if (SIDE1) columns(0);
         ok = ok && w.wait_warp(smem_u32(&sh->sum_full[buf]), (it >> 1) & 1);
         tc_fence_after();
-        if (ok) {
-          const uint32_t from = tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256 + h * 128;
-          uint32_t r[2][16];
-          tmem_ld16(from, r[0]);
+        uint32_t r[2][16];
+        tmem_ld16(from, r[0]);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            tmem_ld_wait();
-            landed(r[c & 1]);
-            if (c < 7) tmem_ld16(from + 16 * (c + 1), r[(c + 1) & 1]);
+        for (int c = 0; c < 8; ++c) {
+          tmem_ld_wait();
+          if (c < 7) {
+            if (SIDE1) columns(c + 1);
+            tmem_ld16(from + 16 * (c + 1), r[(c + 1) & 1]);
+          } else {                                                            // all of it is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->sum_empty[buf]), 0));
+          }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              uint64_t v = pair_of(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1]));
-              if (SIDE1) v = mul2(v, *reinterpret_cast<const uint64_t*>(&sh->dw[buf][h * 128 + 16 * c + 2 * i]));
-              acc[8 * c + i] = fma2(v, scale, acc[8 * c + i]);
-            }
+          for (int i = 0; i < 8; ++i) {
+            const float4& e = d[c & 1][SIDE1 ? i / 2 : 0];
+            if (SIDE1) add_scaled(acc[8 * c + i], r[c & 1][2 * i], r[c & 1][2 * i + 1], i & 1 ? pair_of(e.z, e.w) : pair_of(e.x, e.y), scale);
+            else add_scaled(acc[8 * c + i], r[c & 1][2 * i], r[c & 1][2 * i + 1], scale);
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->sum_empty[buf]), 0));
       }
 #pragma unroll
       for (int ch = 0; ch < 128 / kChunk; ++ch) {
@@ -602,7 +646,7 @@ Plan make_plan(const LinearFp8Args& l, bool aligned) {
 }
 
 constexpr size_t kFewRing = 200 * 1024;
-constexpr size_t kFewSmem = 1024 + kFewRing + sizeof(SharedFew);
+constexpr size_t kFewSmem = 1024 + kFewRing + few_scale_bytes(128) + sizeof(SharedFew);
 
 template <typename T, int NT>
 qm_status launch_few(const LinearFp8Args& l, int split, cudaStream_t s) {
@@ -619,7 +663,7 @@ qm_status launch_few(const LinearFp8Args& l, int split, cudaStream_t s) {
   // as in the INT8 product: half an SM's shared memory for a part that is on its way at once anyhow
   const size_t blocks = (size_t)((a.num_kb + split - 1) / split), ring = blocks * stage;
   const bool shortly = ring <= 160 * 1024;
-  a.stages = (int)std::min<size_t>({(size_t)kFewStages, blocks, (shortly ? kFewRing / 2 - std::min<size_t>(a.sums_bytes, kFewRing / 4) : kFewRing - a.sums_bytes) / stage});
+  a.stages = (int)std::min<size_t>({(size_t)kFewStages, blocks, (shortly ? kFewRing / 2 - 10240 - std::min<size_t>(a.sums_bytes, kFewRing / 4) : kFewRing - a.sums_bytes) / stage});
   a.prefetch = l.N * l.K >= (32ll << 20) ? 4 : 0;
   a.tiles_m = (int)tiles_m;
   a.idesc = idesc_of(l.fmt_w, l.fmt_x, kBlock, NT);
@@ -628,7 +672,7 @@ qm_status launch_few(const LinearFp8Args& l, int split, cudaStream_t s) {
   wait_settings(&a.waits.limit_ns, &a.waits.stop_after);
   CUtensorMap maps[2];
   if (!code_map(&maps[0], l.x, l.K, l.M, l.ld_x, NT) || !code_map(&maps[1], l.w, l.K, l.N, l.ld_w, kBlock)) return QM_ERR_CUDA;
-  const size_t smem = 1024 + a.stages * stage + a.sums_bytes + sizeof(SharedFew);
+  const size_t smem = 1024 + a.stages * stage + a.sums_bytes + few_scale_bytes(NT) + sizeof(SharedFew);
   return launch_cluster(linear_fp8_few<T, NT>, ready, smem, kFewSmem, (unsigned)(tiles * split), kThreads, (unsigned)split, s, maps[0], maps[1], a);
 }
 
@@ -637,7 +681,7 @@ qm_status launch_many(const LinearFp8Args& l, cudaStream_t s) {
   static std::atomic<bool> ready[kMaxDevices];
   // all of an SM's shared memory: a CTA that holds tensor memory waits for its peer here, so neither may have to wait for another kernel's
   constexpr size_t smem = 232448;
-  static_assert(1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + sizeof(SharedMany) <= smem, "shared memory of a CTA");
+  static_assert(1024 + (size_t)kManyStages * kManyStageBytes + kEpiWarps * kOutBytes + many_scale_bytes(SIDE1) + sizeof(SharedMany) <= smem, "shared memory of a CTA");
   ManyArgs a{};
   a.M = l.M; a.N = l.N;
   a.num_kb = (int)((l.K + kBlock - 1) / kBlock);

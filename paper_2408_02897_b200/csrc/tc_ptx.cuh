@@ -196,12 +196,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// What a wait has brought, said to the compiler: nothing that uses it moves ahead of the wait.
-__device__ __forceinline__ void landed(uint32_t (&r)[16]) {
-#pragma unroll
-  for (int i = 0; i < 16; i += 4) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]));
-}
-
 // Instruction descriptor: D format [4,6), A format [7,10), B format [10,13), majors [15],[16]
 // (0 = contraction-major), N/8 at [17,23), M/16 at [24,29).
 __host__ __device__ constexpr uint32_t make_idesc(uint32_t c_fmt, uint32_t a_fmt, uint32_t b_fmt,
