@@ -12,6 +12,9 @@
 // thread loads 16 bytes of keys or values straight from the cache in the places that the instruction's operands have, so nothing goes through
 // shared memory. A thread block takes an equal share of the cells (32 tokens for 16 rows and a head) of all sequences together, wherever they begin
 // and end; what is left of rows whose keys were shared out is joined by attention_join, in the order of the keys.
+//
+// attention_tiles, for sequences with many query rows: 128 of them to a thread block, 16 a warp. Tiles of 64 keys and values are turned into fp16
+// in shared memory once for all of its warps, the next tile's codes on their way meanwhile.
 #include <algorithm>
 #include <atomic>
 
@@ -30,6 +33,7 @@ struct RowsArgs {
   float scale_log2;                              // of scores to the base 2
   __nv_bfloat16* out; int64_t ld_out;
   float* lse;
+  int most_rows;                                 // sequences with as many query rows of a cached head or more are attention_tiles'
   struct Share* shares;                          // one a thread block
   float* parts;                                  // [2 * blocks][16][padded dim + 2]
 };
@@ -50,6 +54,12 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return r;
 }
 
+// The power of two that brings a row's largest magnitude to 2^14 .. 2^15 (1 where that is 0 or not finite).
+__device__ __forceinline__ float row_scale(float top) {
+  const int ex = (int)(__float_as_uint(top) >> 23) - 127;
+  return __uint_as_float((uint32_t)(127 + (top == 0.f || ex == 128 ? 0 : max(min(14 - ex, 120), -126))) << 23);
+}
+
 template <int N> struct Words { uint32_t w[N]; };
 __device__ __forceinline__ Words<4> load_words(const uint8_t* p, Words<4>) {
   Words<4> r;
@@ -63,7 +73,7 @@ __device__ __forceinline__ Words<2> load_words(const uint8_t* p, Words<2>) {
 }
 
 __device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e) {
-  if (e.n == 0) return 0;
+  if (e.n == 0 || (int64_t)e.n * a.group >= a.most_rows) return 0;
   return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.len + kCell - 1) / kCell);
 }
 
@@ -156,11 +166,8 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
           }
           top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
           top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-          // the power of two that brings the row's largest magnitude to 2^14 .. 2^15
-          const int ex = (int)(__float_as_uint(top[r]) >> 23) - 127;
-          const int up = top[r] == 0.f || ex == 128 ? 0 : min(14 - ex, 120);
-          const float by = __uint_as_float((uint32_t)(127 + max(up, -126)) << 23);
-          factor[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - max(up, -126)) << 23);
+          const float by = row_scale(top[r]);
+          factor[r] = a.scale_log2 / by;
 #pragma unroll
           for (int s = 0; s < 4 * kChunks; ++s) {
             q[s][r] = pack_half2(bf16_lo(raw[r][s].x) * by, bf16_hi(raw[r][s].x) * by);
@@ -400,6 +407,232 @@ __global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid
   }
 }
 
+// ---------------------------------------------------------------- many rows
+constexpr int kTileRows = 128, kTileKeys = 64;
+// keys and values of a tile; bytes between tokens that put eight rows on distinct banks
+template <int DIM> __host__ __device__ constexpr uint32_t tile_bytes() { return 2u * kTileKeys * (DIM * 2 + 16); }
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_turned(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+template <int FMT, int DIM>
+__global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int64_t candidates) {
+  constexpr int kPitch = DIM * 2 + 16, kSteps = DIM / 16, kOut = DIM / 8;
+  constexpr int kPieces = kTileKeys * (DIM / 16) / 256;                        // 16-byte pieces of a tile's keys in a thread
+  extern __shared__ __align__(16) uint8_t tile_raw[];                          // [2 buffers][keys, values][64][kPitch]
+  __shared__ float scales[2][2][4];                                            // [buffer][keys, values][16 tokens]
+  pdl_prologue();
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
+  // Sequence b has the candidates from starts[b] group / 128 + b on, at least as many as its tiles.  The last ones, which see most, come first.
+  const int head = blockIdx.y;
+  const int64_t cand = candidates - 1 - blockIdx.x;
+  auto from_of = [&](int i) { return (int64_t)(c.starts ? c.starts[i] : i) * a.group / kTileRows + i; };
+  int lo = 0, hi = c.batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (from_of(mid) <= cand) lo = mid; else hi = mid - 1;
+  }
+  const int b = lo;
+  const Extent e = extent_of(c, b);
+  const int64_t row0 = (cand - from_of(b)) * kTileRows, all = (int64_t)e.n * a.group;
+  if (all < a.most_rows || row0 < 0 || row0 >= all) return;
+
+  const int first = (int)row0 + 16 * warp, rows = min(16, (int)all - first);   // of this warp; may be below 1
+  auto limit_of = [&](int64_t r) { return r < all ? max(0, e.len - e.n + (int)(r / a.group) + 1) : 0; };
+  const int limit[2] = {limit_of(first + g), limit_of(first + g + 8)};
+  const int least = rows > 0 ? limit_of(first) : 0, most = rows > 0 ? limit_of(first + rows - 1) : 0;
+  const int seen = limit_of(min(row0 + kTileRows, all) - 1), tiles = (seen + kTileKeys - 1) / kTileKeys;      // by the whole block
+
+  uint32_t q[kSteps][4];
+  float factor[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int64_t row = first + g + 8 * r, token = row / a.group;
+    const bool in = g + 8 * r < rows;
+    const __nv_bfloat16* const from = a.q + (e.first + (in ? token : 0)) * a.ld_q + ((int64_t)head * a.group + (in ? row - token * a.group : 0)) * c.dim;
+    uint32_t raw[kSteps][2];
+    float top = 0.f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int d = 16 * s + 8 * i + 2 * cc;
+        raw[s][i] = in && d < c.dim ? *reinterpret_cast<const uint32_t*>(from + d) : 0u;
+        top = fmaxf(top, fmaxf(fabsf(bf16_lo(raw[s][i])), fabsf(bf16_hi(raw[s][i]))));
+      }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const float by = row_scale(top);
+    factor[r] = a.scale_log2 / by;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      q[s][r] = pack_half2(bf16_lo(raw[s][0]) * by, bf16_hi(raw[s][0]) * by);
+      q[s][2 + r] = pack_half2(bf16_lo(raw[s][1]) * by, bf16_hi(raw[s][1]) * by);
+    }
+  }
+
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float o[kOut][4];
+#pragma unroll
+  for (int t = 0; t < kOut; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
+
+  // ---- a tile's codes: in registers, then as fp16 in shared memory
+  Words<4> k[kPieces], v[kPieces];
+  float scale = 0.f;
+  int page[kPieces], page_s = -1;
+  auto token_of = [&](int i) { return (tid + 256 * i) / (DIM / 16); };
+  auto pages = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int token = tile * kTileKeys + token_of(i);
+      page[i] = token < seen ? page_of(c, b, token >> c.shift) : -1;
+    }
+    const int token = tile * kTileKeys + 16 * (tid & 3);
+    page_s = tid < 8 && token < seen ? page_of(c, b, token >> c.shift) : -1;
+  };
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int token = tile * kTileKeys + token_of(i), d = (tid + 256 * i) % (DIM / 16) * 16;
+      const bool in = page[i] >= 0 && d < c.dim;                               // (nothing behind the last key that is seen: its codes may be anything)
+      const int64_t at = ((((int64_t)(in ? page[i] : 0) * c.kv_heads + head) << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim + d;
+      k[i] = in ? load_words(c.k + at, Words<4>()) : Words<4>{};
+      v[i] = in ? load_words(c.v + at, Words<4>()) : Words<4>{};
+    }
+    if (tid < 8) scale = page_s >= 0 ? __ldg((tid < 4 ? c.dk : c.dv) + (int64_t)page_s * c.kv_heads + head) : __int_as_float(0x7fffffff);
+  };
+  const uint32_t smem = (uint32_t)__cvta_generic_to_shared(tile_raw);
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t at = smem + buf * tile_bytes<DIM>() + token_of(i) * kPitch + (tid + 256 * i) % (DIM / 16) * 32;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const Words<4>& w = x ? v[i] : k[i];
+        uint32_t h[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) half4_of<FMT>(w.w[j], h[2 * j], h[2 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + x * kTileKeys * kPitch + 16 * j), "r"(h[4 * j]), "r"(h[4 * j + 1]),
+                       "r"(h[4 * j + 2]), "r"(h[4 * j + 3]) : "memory");
+      }
+    }
+    if (tid < 8) scales[buf][tid >> 2][tid & 3] = scale;
+  };
+  pages(0);
+  load(0);
+  pages(1);
+  store(0);
+  __syncthreads();
+  const uint32_t at_k = (lane & 7) * kPitch + (lane >> 4) * 8 * kPitch + ((lane >> 3) & 1) * 16;
+  const uint32_t at_v = (lane & 7) * kPitch + ((lane >> 3) & 1) * 8 * kPitch + (lane >> 4) * 16;
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int buf = tile & 1;
+    if (tile + 1 < tiles) { load(tile + 1); pages(tile + 2); }
+    if (tile * kTileKeys < most) {                                             // (uniform in the warp)
+      const uint32_t keys = smem + buf * tile_bytes<DIM>(), values = keys + kTileKeys * kPitch;
+      float s[8][4];
+#pragma unroll
+      for (int t = 0; t < 8; t += 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] = s[t + 1][i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kSteps; ++d) {
+          uint32_t r[4];
+          ldmatrix4(r, keys + at_k + t * 8 * kPitch + d * 32);
+          mma16(s[t], q[d], r[0], r[1]);
+          mma16(s[t + 1], q[d], r[2], r[3]);
+        }
+      }
+      float top[2] = {m[0], m[1]};
+      float weigh[4], inverse[4], cv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        cv[i] = scales[buf][1][i];
+        const bool tiny = cv[i] < kLeastScale;
+        weigh[i] = tiny ? -60.f : lg2(cv[i]);
+        inverse[i] = tiny ? 1.1529215e18f : __frcp_rn(cv[i]);
+      }
+      const bool partial = (tile + 1) * kTileKeys > least;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float ck = scales[buf][0][t >> 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = i >> 1;
+          s[t][i] = fmaf(s[t][i], factor[r] * ck, weigh[t >> 1]);
+          if (partial && tile * kTileKeys + 8 * t + 2 * cc + (i & 1) >= limit[r]) s[t][i] = -INFINITY;
+          top[r] = fmaxf(top[r], s[t][i]);
+        }
+      }
+      bool moved = false;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+        moved |= top[r] > m[r];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float shrink = m[r] == top[r] ? 1.f : ex2(m[r] - top[r]);
+          m[r] = top[r];
+          l[r] *= shrink;
+#pragma unroll
+          for (int t = 0; t < kOut; ++t) { o[t][2 * r] *= shrink; o[t][2 * r + 1] *= shrink; }
+        }
+      }
+      float base[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) base[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                                            // 16 keys
+        uint32_t p[4];
+        const bool none = cv[i] < kLeastScale;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float e0 = ex2(s[2 * i][2 * r] - base[r]), e1 = ex2(s[2 * i][2 * r + 1] - base[r]);
+          const float e2 = ex2(s[2 * i + 1][2 * r] - base[r]), e3 = ex2(s[2 * i + 1][2 * r + 1] - base[r]);
+          const float sum = (e0 + e1) + (e2 + e3);
+          if (sum != 0.f) l[r] = fmaf(sum, inverse[i], l[r]);
+          p[r] = none ? 0u : pack_half2(e0, e1);
+          p[2 + r] = none ? 0u : pack_half2(e2, e3);
+        }
+#pragma unroll
+        for (int t = 0; t < kOut; t += 2) {
+          uint32_t w[4];
+          ldmatrix4_turned(w, values + at_v + i * 16 * kPitch + t * 16);
+          mma16(o[t], p, w[0], w[1]);
+          mma16(o[t + 1], p, w[2], w[3]);
+        }
+      }
+    }
+    if (tile + 1 < tiles) store(buf ^ 1);                                      // (the tile before this one has been read by all: the barrier below)
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+    if (g + 8 * r >= rows) continue;
+    const int64_t row = first + g + 8 * r, token = row / a.group, h = (int64_t)head * a.group + row - token * a.group;
+    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+    __nv_bfloat16* const to = a.out + (e.first + token) * a.ld_out + h * c.dim;
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+      if (8 * t < c.dim) *reinterpret_cast<uint32_t*>(to + 8 * t + 2 * cc) = pack_bf16x2(o[t][2 * r] * inv, o[t][2 * r + 1] * inv);
+    if (cc == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = l[r] == 0.f ? -INFINITY : (log2f(l[r]) + (m[r] - 14.f)) * 0.69314718f;
+  }
+}
+
 constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + 255) / 256 * 256; }
 
 template <int FMT, int DIM>
@@ -424,8 +657,36 @@ qm_status launch_rows(RowsArgs a, cudaStream_t s) {
   }
   return QM_OK;
 }
+template <int FMT, int DIM>
+qm_status launch_tiles(const RowsArgs& a, cudaStream_t s) {
+  constexpr auto kern = attention_tiles<FMT, DIM>;
+  static std::atomic<bool> ready[kMaxDevices];
+  const int dev = current_device();
+  if (dev < 0) return QM_ERR_UNSUPPORTED;
+  if (!ready[dev].load(std::memory_order_relaxed)) {
+    QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * tile_bytes<DIM>())));
+    ready[dev].store(true, std::memory_order_relaxed);
+  }
+  const int64_t candidates = a.c.tokens * a.group / kTileRows + a.c.batch;
+  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)candidates, (unsigned)a.c.kv_heads), dim3(256), 2 * tile_bytes<DIM>(), s, a, candidates));
+  count_launch();
+  return QM_OK;
+}
+
+// Which sequences are whose: attention_tiles takes those with 64 query rows of a cached head or more, if the call has enough of them to give a third
+// of the SMs 128 rows; its thread blocks do not share keys, attention_rows does, whatever the rows.
+template <int FMT, int DIM>
+qm_status launch_both(RowsArgs a, cudaStream_t s) {
+  const bool tiles = (a.c.tokens - a.c.batch + 1) * a.group >= 64 && a.c.tokens * a.group / kTileRows * a.c.kv_heads >= sm_count() / 3 && a.c.kv_heads < 65536;
+  a.most_rows = tiles ? 64 : 0x7fffffff;
+  if (tiles) {
+    const qm_status st = launch_tiles<FMT, DIM>(a, s);
+    if (st != QM_OK) return st;
+  }
+  return launch_rows<FMT, DIM>(a, s);
+}
 template <int FMT>
-qm_status launch_dim(const RowsArgs& a, cudaStream_t s) { return a.c.dim <= 64 ? launch_rows<FMT, 64>(a, s) : launch_rows<FMT, 128>(a, s); }
+qm_status launch_dim(const RowsArgs& a, cudaStream_t s) { return a.c.dim <= 64 ? launch_both<FMT, 64>(a, s) : launch_both<FMT, 128>(a, s); }
 
 }  // namespace
 

@@ -352,3 +352,42 @@ def test_tokens_generated_one_by_one(fmt):
         # a rounding is off by half a step: of int8 half a scale, of FP8 half a step of the value or of the least normal one; rounded again a few times
         step = {"int8": 0.5 * case.dv.max(), "e4m3": 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * case.dv.max(), "e5m2": 2.0 ** -3 * np.abs(x) + 2.0 ** -17 * case.dv.max()}[fmt]
         assert (np.abs(held - x) <= 6 * step).all() and math.isfinite(float(np.abs(held).max()))
+
+
+# Sequences of 64 query rows of a cached head and more, in calls with many of them (the kernel for 128 rows at a time), beside shorter ones.
+TILED = [(16, 2, 64, 16), (20, 1, 128, 64), (16, 3, 80, 32), (24, 4, 48, 128), (17, 8, 96, 256)]
+
+
+@pytest.mark.parametrize("kv,group,dim,block", TILED)
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_tiles(kv, group, dim, block, fmt):
+    new = [130, 1, 0, 257, 64, 7, 40]
+    lens = [130, 300, 9, 400, 65, 100, 39]                        # (of the last one, a token lies below position 0)
+    check_attention(Case(fmt, kv, dim, block, new, lens, seed=block + dim).fill(lens), kv * group)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_tiles_of_values_far_apart_in_scale(fmt):
+    lens, new = [300, 150], [200, 100]
+    case = Case(fmt, 16, 64, 16, new, lens, seed=3).fill(lens)
+    held = np.isfinite(case.dv)
+    spread = np.exp(case.rng.uniform(-25, 25, case.dv.shape)) * (case.rng.random(case.dv.shape) < 0.8)
+    case.dv[held] = (case.dv * spread)[held].astype(np.float32)
+    check_attention(case, 32)
+
+
+def test_tiles_nan_and_bad_blocks():
+    lens, new = [200, 180], [200, 180]
+    case = Case("int8", 16, 64, 16, new, lens, seed=2).fill(lens)
+    sound = run_attention(case, 32)[1]
+    bad = Case("int8", 16, 64, 16, new, lens, seed=2).fill(lens)
+    page = bad.tables[0, 5]                                       # positions 80 .. 95 of sequence 0, head 1
+    bad.dv[page, 1] = np.nan
+    bad.v[page, 1] = 0
+    bad.tables[1, 2] = len(bad.k)                                 # positions 32 .. 47 of sequence 1
+    out = run_attention(bad, 32)[1]
+    sees = np.zeros(out.shape[:2], bool)
+    sees[80:200, 2:4] = True
+    sees[200 + 32:] = True
+    assert np.array_equal(np.isnan(out).all(2), sees) and np.array_equal(np.isnan(out).any(2), sees)
+    assert np.array_equal(out[~sees], sound[~sees])
