@@ -45,7 +45,7 @@ __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
@@ -539,17 +539,24 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
     if (tile + 1 < tiles) { load(tile + 1); pages(tile + 2); }
     if (tile * kTileKeys < most) {                                             // (uniform in the warp)
       const uint32_t keys = smem + buf * tile_bytes<DIM>(), values = keys + kTileKeys * kPitch;
+      // (16 dims of all 64 keys at a time, the next ones' operands on their way: eight products that do not wait for one another)
       float s[8][4];
 #pragma unroll
-      for (int t = 0; t < 8; t += 2) {
+      for (int t = 0; t < 8; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] = s[t + 1][i] = 0.f;
+        for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
+      uint32_t w[2][4][4];
 #pragma unroll
-        for (int d = 0; d < kSteps; ++d) {
-          uint32_t r[4];
-          ldmatrix4(r, keys + at_k + t * 8 * kPitch + d * 32);
-          mma16(s[t], q[d], r[0], r[1]);
-          mma16(s[t + 1], q[d], r[2], r[3]);
+      for (int t = 0; t < 4; ++t) ldmatrix4(w[0][t], keys + at_k + t * 16 * kPitch);
+#pragma unroll
+      for (int d = 0; d < kSteps; ++d) {
+        if (d + 1 < kSteps)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) ldmatrix4(w[(d + 1) & 1][t], keys + at_k + t * 16 * kPitch + (d + 1) * 32);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          mma16(s[2 * t], q[d], w[d & 1][t][0], w[d & 1][t][1]);
+          mma16(s[2 * t + 1], q[d], w[d & 1][t][2], w[d & 1][t][3]);
         }
       }
       float top[2] = {m[0], m[1]};
@@ -593,6 +600,13 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
       float base[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) base[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
+      constexpr int kHalves = kOut / 8;                                        // of the output, 64 dims each
+      auto operands = [&](int step) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          ldmatrix4_turned(w[step & 1][t], values + at_v + step / kHalves * 16 * kPitch + (step % kHalves * 4 + t) * 32);
+      };
+      operands(0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {                                            // 16 keys
         uint32_t p[4];
@@ -607,11 +621,14 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
           p[2 + r] = none ? 0u : pack_half2(e2, e3);
         }
 #pragma unroll
-        for (int t = 0; t < kOut; t += 2) {
-          uint32_t w[4];
-          ldmatrix4_turned(w, values + at_v + i * 16 * kPitch + t * 16);
-          mma16(o[t], p, w[0], w[1]);
-          mma16(o[t + 1], p, w[2], w[3]);
+        for (int h = 0; h < kHalves; ++h) {
+          const int step = i * kHalves + h;
+          if (step + 1 < 4 * kHalves) operands(step + 1);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            mma16(o[8 * h + 2 * t], p, w[step & 1][t][0], w[step & 1][t][1]);
+            mma16(o[8 * h + 2 * t + 1], p, w[step & 1][t][2], w[step & 1][t][3]);
+          }
         }
       }
     }
