@@ -13,7 +13,7 @@
 // shared memory. A thread block takes an equal share of the cells (32 tokens for 16 rows and a head) of all sequences together, wherever they begin
 // and end; what is left of rows whose keys were shared out is joined by attention_join, in the order of the keys.
 //
-// attention_tiles, for sequences with many query rows: 128 of them to a thread block, 16 a warp. Tiles of 64 keys and values are turned into fp16
+// attention_tiles, for sequences with many query rows: 128 or 256 of them to a thread block. Tiles of 32 keys and values are turned into fp16
 // in shared memory once for all of its warps, the next tile's codes on their way meanwhile.
 #include <algorithm>
 #include <atomic>
@@ -408,9 +408,10 @@ __global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid
 }
 
 // ---------------------------------------------------------------- many rows
-constexpr int kTileRows = 128, kTileKeys = 64;
+constexpr int kTileKeys = 32, kGroups = kTileKeys / 16;
 // keys and values of a tile; bytes between tokens that put eight rows on distinct banks
 template <int DIM> __host__ __device__ constexpr uint32_t tile_bytes() { return 2u * kTileKeys * (DIM * 2 + 16); }
+template <int DIM> __host__ __device__ constexpr uint32_t tiles_smem(int mt) { return 2 * tile_bytes<DIM>() + 128 * mt * (DIM * 2 + 16); }
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -419,16 +420,18 @@ __device__ __forceinline__ void ldmatrix4_turned(uint32_t (&r)[4], uint32_t addr
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
-template <int FMT, int DIM>
-__global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int64_t candidates) {
-  constexpr int kPitch = DIM * 2 + 16, kSteps = DIM / 16, kOut = DIM / 8;
-  constexpr int kPieces = kTileKeys * (DIM / 16) / 256;                        // 16-byte pieces of a tile's keys in a thread
-  extern __shared__ __align__(16) uint8_t tile_raw[];                          // [2 buffers][keys, values][64][kPitch]
-  __shared__ float scales[2][2][4];                                            // [buffer][keys, values][16 tokens]
+// MT: times 16 rows a warp.  An operand of keys or values is 256 bytes of shared memory for a product of eight cycles a scheduler, which with 16 rows
+// is all that shared memory gives; 32 rows use it twice.
+template <int FMT, int DIM, int MT>
+__global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const RowsArgs a, int64_t candidates) {
+  constexpr int kTileRows = 128 * MT, kPitch = DIM * 2 + 16, kSteps = DIM / 16, kOut = DIM / 8;
+  static_assert(kTileKeys * DIM / 16 <= 256, "a 16-byte piece of the keys to a thread");
+  extern __shared__ __align__(16) uint8_t tile_raw[];                          // [2 buffers][keys, values][kTileKeys][kPitch], queries [kTileRows][kPitch]
+  __shared__ float scales[2][2][kGroups];                                         // [buffer][keys, values][16 tokens]
   pdl_prologue();
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
-  // Sequence b has the candidates from starts[b] group / 128 + b on, at least as many as its tiles.  The last ones, which see most, come first.
+  // Sequence b has the candidates from starts[b] group / kTileRows + b on, at least as many as its tiles.  The last ones, which see most, come first.
   const int head = blockIdx.y;
   const int64_t cand = candidates - 1 - blockIdx.x;
   auto from_of = [&](int i) { return (int64_t)(c.starts ? c.starts[i] : i) * a.group / kTileRows + i; };
@@ -442,80 +445,86 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
   const int64_t row0 = (cand - from_of(b)) * kTileRows, all = (int64_t)e.n * a.group;
   if (all < a.most_rows || row0 < 0 || row0 >= all) return;
 
-  const int first = (int)row0 + 16 * warp, rows = min(16, (int)all - first);   // of this warp; may be below 1
   auto limit_of = [&](int64_t r) { return r < all ? max(0, e.len - e.n + (int)(r / a.group) + 1) : 0; };
-  const int limit[2] = {limit_of(first + g), limit_of(first + g + 8)};
-  const int least = rows > 0 ? limit_of(first) : 0, most = rows > 0 ? limit_of(first + rows - 1) : 0;
+  const int64_t first = row0 + 16 * MT * warp;                                 // of this warp; may be beyond the last
+  const int rows = (int)min((int64_t)16 * MT, all - first);
+  int limit[MT][2];
+#pragma unroll
+  for (int u = 0; u < MT; ++u)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) limit[u][r] = limit_of(first + 16 * u + 8 * r + g);
+  const int least = rows > 0 ? limit_of(first + 16 * MT - 1 < all ? first : all) : 0;      // (a row beyond the last sees nothing)
+  const int most = rows > 0 ? limit_of(first + rows - 1) : 0;
   const int seen = limit_of(min(row0 + kTileRows, all) - 1), tiles = (seen + kTileKeys - 1) / kTileKeys;      // by the whole block
 
-  uint32_t q[kSteps][4];
-  float factor[2];
+  const uint32_t smem = (uint32_t)__cvta_generic_to_shared(tile_raw), queries = smem + 2 * tile_bytes<DIM>() + warp * 16 * MT * kPitch;      // the warp's
+  float factor[MT][2];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int64_t row = first + g + 8 * r, token = row / a.group;
-    const bool in = g + 8 * r < rows;
-    const __nv_bfloat16* const from = a.q + (e.first + (in ? token : 0)) * a.ld_q + ((int64_t)head * a.group + (in ? row - token * a.group : 0)) * c.dim;
-    uint32_t raw[kSteps][2];
-    float top = 0.f;
+  for (int u = 0; u < MT; ++u)
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
+    for (int r = 0; r < 2; ++r) {
+      const int in_warp = 16 * u + 8 * r + g;
+      const int64_t row = first + in_warp, token = row / a.group;
+      const bool in = in_warp < rows;
+      const __nv_bfloat16* const from = a.q + (e.first + (in ? token : 0)) * a.ld_q + ((int64_t)head * a.group + (in ? row - token * a.group : 0)) * c.dim;
+      uint32_t raw[kSteps][2];
+      float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int d = 16 * s + 8 * i + 2 * cc;
-        raw[s][i] = in && d < c.dim ? *reinterpret_cast<const uint32_t*>(from + d) : 0u;
-        top = fmaxf(top, fmaxf(fabsf(bf16_lo(raw[s][i])), fabsf(bf16_hi(raw[s][i]))));
-      }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const float by = row_scale(top);
-    factor[r] = a.scale_log2 / by;
+      for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      q[s][r] = pack_half2(bf16_lo(raw[s][0]) * by, bf16_hi(raw[s][0]) * by);
-      q[s][2 + r] = pack_half2(bf16_lo(raw[s][1]) * by, bf16_hi(raw[s][1]) * by);
+        for (int i = 0; i < 2; ++i) {
+          const int d = 16 * s + 8 * i + 2 * cc;
+          raw[s][i] = in && d < c.dim ? *reinterpret_cast<const uint32_t*>(from + d) : 0u;
+          top = fmaxf(top, fmaxf(fabsf(bf16_lo(raw[s][i])), fabsf(bf16_hi(raw[s][i]))));
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float by = row_scale(top);
+      factor[u][r] = a.scale_log2 / by;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(queries + in_warp * kPitch + s * 32 + i * 16 + cc * 4),
+                       "r"(pack_half2(bf16_lo(raw[s][i]) * by, bf16_hi(raw[s][i]) * by)) : "memory");
     }
+  __syncwarp();
+
+  float m[MT][2], l[MT][2], o[MT][kOut][4];
+#pragma unroll
+  for (int u = 0; u < MT; ++u) {
+    m[u][0] = m[u][1] = -INFINITY;
+    l[u][0] = l[u][1] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[u][t][i] = 0.f;
   }
 
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  float o[kOut][4];
-#pragma unroll
-  for (int t = 0; t < kOut; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
-
   // ---- a tile's codes: in registers, then as fp16 in shared memory
-  Words<4> k[kPieces], v[kPieces];
+  Words<4> k, v;
   float scale = 0.f;
-  int page[kPieces], page_s = -1;
-  auto token_of = [&](int i) { return (tid + 256 * i) / (DIM / 16); };
+  int page, page_s = -1;
+  const int token_in = tid / (DIM / 16), dim_in = tid % (DIM / 16) * 16;       // this thread's piece
   auto pages = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int token = tile * kTileKeys + token_of(i);
-      page[i] = token < seen ? page_of(c, b, token >> c.shift) : -1;
-    }
-    const int token = tile * kTileKeys + 16 * (tid & 3);
-    page_s = tid < 8 && token < seen ? page_of(c, b, token >> c.shift) : -1;
+    const int token = tile * kTileKeys + token_in, group = tile * kTileKeys + 16 * (tid % kGroups);
+    page = token_in < kTileKeys && token < seen ? page_of(c, b, token >> c.shift) : -1;
+    page_s = tid < 2 * kGroups && group < seen ? page_of(c, b, group >> c.shift) : -1;
   };
   auto load = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int token = tile * kTileKeys + token_of(i), d = (tid + 256 * i) % (DIM / 16) * 16;
-      const bool in = page[i] >= 0 && d < c.dim;                               // (nothing behind the last key that is seen: its codes may be anything)
-      const int64_t at = ((((int64_t)(in ? page[i] : 0) * c.kv_heads + head) << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim + d;
-      k[i] = in ? load_words(c.k + at, Words<4>()) : Words<4>{};
-      v[i] = in ? load_words(c.v + at, Words<4>()) : Words<4>{};
-    }
-    if (tid < 8) scale = page_s >= 0 ? __ldg((tid < 4 ? c.dk : c.dv) + (int64_t)page_s * c.kv_heads + head) : __int_as_float(0x7fffffff);
+    const int token = tile * kTileKeys + token_in;
+    const bool in = page >= 0 && dim_in < c.dim;                               // (nothing behind the last key that is seen: its codes may be anything)
+    const int64_t at = ((((int64_t)(in ? page : 0) * c.kv_heads + head) << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim + dim_in;
+    k = in ? load_words(c.k + at, Words<4>()) : Words<4>{};
+    v = in ? load_words(c.v + at, Words<4>()) : Words<4>{};
+    if (tid < 2 * kGroups) scale = page_s >= 0 ? __ldg((tid < kGroups ? c.dk : c.dv) + (int64_t)page_s * c.kv_heads + head) : __int_as_float(0x7fffffff);
   };
-  const uint32_t smem = (uint32_t)__cvta_generic_to_shared(tile_raw);
   auto store = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const uint32_t at = smem + buf * tile_bytes<DIM>() + token_of(i) * kPitch + (tid + 256 * i) % (DIM / 16) * 32;
+    const uint32_t at = smem + buf * tile_bytes<DIM>() + token_in * kPitch + dim_in * 2;
+    if (token_in < kTileKeys)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const Words<4>& w = x ? v[i] : k[i];
+        const Words<4>& w = x ? v : k;
         uint32_t h[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) half4_of<FMT>(w.w[j], h[2 * j], h[2 * j + 1]);
@@ -524,14 +533,14 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + x * kTileKeys * kPitch + 16 * j), "r"(h[4 * j]), "r"(h[4 * j + 1]),
                        "r"(h[4 * j + 2]), "r"(h[4 * j + 3]) : "memory");
       }
-    }
-    if (tid < 8) scales[buf][tid >> 2][tid & 3] = scale;
+    if (tid < 2 * kGroups) scales[buf][tid / kGroups][tid % kGroups] = scale;
   };
   pages(0);
   load(0);
   pages(1);
   store(0);
   __syncthreads();
+  const uint32_t at_q = queries + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
   const uint32_t at_k = (lane & 7) * kPitch + (lane >> 4) * 8 * kPitch + ((lane >> 3) & 1) * 16;
   const uint32_t at_v = (lane & 7) * kPitch + ((lane >> 3) & 1) * 8 * kPitch + (lane >> 4) * 16;
   for (int tile = 0; tile < tiles; ++tile) {
@@ -539,115 +548,121 @@ __global__ void __launch_bounds__(256, 1) attention_tiles(const RowsArgs a, int6
     if (tile + 1 < tiles) { load(tile + 1); pages(tile + 2); }
     if (tile * kTileKeys < most) {                                             // (uniform in the warp)
       const uint32_t keys = smem + buf * tile_bytes<DIM>(), values = keys + kTileKeys * kPitch;
-      // (16 dims of all 64 keys at a time, the next ones' operands on their way: eight products that do not wait for one another)
-      float s[8][4];
+      // (16 dims of all keys at a time: products that do not wait for one another)
+      float s[MT][2 * kGroups][4];
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
+      for (int u = 0; u < MT; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
-      uint32_t w[2][4][4];
+        for (int t = 0; t < 2 * kGroups; ++t)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) ldmatrix4(w[0][t], keys + at_k + t * 16 * kPitch);
+          for (int i = 0; i < 4; ++i) s[u][t][i] = 0.f;
 #pragma unroll
       for (int d = 0; d < kSteps; ++d) {
-        if (d + 1 < kSteps)
+        uint32_t q[MT][4], w[kGroups][4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) ldmatrix4(w[(d + 1) & 1][t], keys + at_k + t * 16 * kPitch + (d + 1) * 32);
+        for (int u = 0; u < MT; ++u) ldmatrix4(q[u], at_q + u * 16 * kPitch + d * 32);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          mma16(s[2 * t], q[d], w[d & 1][t][0], w[d & 1][t][1]);
-          mma16(s[2 * t + 1], q[d], w[d & 1][t][2], w[d & 1][t][3]);
-        }
+        for (int t = 0; t < kGroups; ++t) ldmatrix4(w[t], keys + at_k + t * 16 * kPitch + d * 32);
+#pragma unroll
+        for (int t = 0; t < kGroups; ++t)
+#pragma unroll
+          for (int u = 0; u < MT; ++u) {
+            mma16(s[u][2 * t], q[u], w[t][0], w[t][1]);
+            mma16(s[u][2 * t + 1], q[u], w[t][2], w[t][3]);
+          }
       }
-      float top[2] = {m[0], m[1]};
-      float weigh[4], inverse[4], cv[4];
+      float weigh[kGroups], inverse[kGroups], cv[kGroups];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kGroups; ++i) {
         cv[i] = scales[buf][1][i];
         const bool tiny = cv[i] < kLeastScale;
         weigh[i] = tiny ? -60.f : lg2(cv[i]);
         inverse[i] = tiny ? 1.1529215e18f : __frcp_rn(cv[i]);
       }
       const bool partial = (tile + 1) * kTileKeys > least;
+      uint32_t p[MT][kGroups][4];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const float ck = scales[buf][0][t >> 1];
+      for (int u = 0; u < MT; ++u) {
+        float top[2] = {m[u][0], m[u][1]};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = i >> 1;
-          s[t][i] = fmaf(s[t][i], factor[r] * ck, weigh[t >> 1]);
-          if (partial && tile * kTileKeys + 8 * t + 2 * cc + (i & 1) >= limit[r]) s[t][i] = -INFINITY;
-          top[r] = fmaxf(top[r], s[t][i]);
+        for (int t = 0; t < 2 * kGroups; ++t) {
+          const float ck = scales[buf][0][t >> 1];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = i >> 1;
+            s[u][t][i] = fmaf(s[u][t][i], factor[u][r] * ck, weigh[t >> 1]);
+            if (partial && tile * kTileKeys + 8 * t + 2 * cc + (i & 1) >= limit[u][r]) s[u][t][i] = -INFINITY;
+            top[r] = fmaxf(top[r], s[u][t][i]);
+          }
         }
-      }
-      bool moved = false;
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-        moved |= top[r] > m[r];
-      }
-      if (__any_sync(0xffffffffu, moved)) {
+        bool moved = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float shrink = m[r] == top[r] ? 1.f : ex2(m[r] - top[r]);
-          m[r] = top[r];
-          l[r] *= shrink;
-#pragma unroll
-          for (int t = 0; t < kOut; ++t) { o[t][2 * r] *= shrink; o[t][2 * r + 1] *= shrink; }
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          moved |= top[r] > m[u][r];
         }
-      }
-      float base[2];
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) base[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
-      constexpr int kHalves = kOut / 8;                                        // of the output, 64 dims each
-      auto operands = [&](int step) {
+          for (int r = 0; r < 2; ++r) {
+            const float shrink = m[u][r] == top[r] ? 1.f : ex2(m[u][r] - top[r]);
+            m[u][r] = top[r];
+            l[u][r] *= shrink;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          ldmatrix4_turned(w[step & 1][t], values + at_v + step / kHalves * 16 * kPitch + (step % kHalves * 4 + t) * 32);
-      };
-      operands(0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {                                            // 16 keys
-        uint32_t p[4];
-        const bool none = cv[i] < kLeastScale;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float e0 = ex2(s[2 * i][2 * r] - base[r]), e1 = ex2(s[2 * i][2 * r + 1] - base[r]);
-          const float e2 = ex2(s[2 * i + 1][2 * r] - base[r]), e3 = ex2(s[2 * i + 1][2 * r + 1] - base[r]);
-          const float sum = (e0 + e1) + (e2 + e3);
-          if (sum != 0.f) l[r] = fmaf(sum, inverse[i], l[r]);
-          p[r] = none ? 0u : pack_half2(e0, e1);
-          p[2 + r] = none ? 0u : pack_half2(e2, e3);
+            for (int t = 0; t < kOut; ++t) { o[u][t][2 * r] *= shrink; o[u][t][2 * r + 1] *= shrink; }
+          }
         }
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-          const int step = i * kHalves + h;
-          if (step + 1 < 4 * kHalves) operands(step + 1);
+        for (int i = 0; i < kGroups; ++i) {
+          const bool none = cv[i] < kLeastScale;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            mma16(o[8 * h + 2 * t], p, w[step & 1][t][0], w[step & 1][t][1]);
-            mma16(o[8 * h + 2 * t + 1], p, w[step & 1][t][2], w[step & 1][t][3]);
+          for (int r = 0; r < 2; ++r) {
+            const float base = m[u][r] == -INFINITY ? 0.f : m[u][r] - 14.f;
+            const float e0 = ex2(s[u][2 * i][2 * r] - base), e1 = ex2(s[u][2 * i][2 * r + 1] - base);
+            const float e2 = ex2(s[u][2 * i + 1][2 * r] - base), e3 = ex2(s[u][2 * i + 1][2 * r + 1] - base);
+            const float sum = (e0 + e1) + (e2 + e3);
+            if (sum != 0.f) l[u][r] = fmaf(sum, inverse[i], l[u][r]);
+            p[u][i][r] = none ? 0u : pack_half2(e0, e1);
+            p[u][i][2 + r] = none ? 0u : pack_half2(e2, e3);
           }
         }
       }
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i)                                        // 16 keys
+#pragma unroll
+        for (int h = 0; h < kOut / 4; ++h) {
+          uint32_t w[2][4];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) ldmatrix4_turned(w[t], values + at_v + i * 16 * kPitch + (2 * h + t) * 32);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int u = 0; u < MT; ++u) {
+              mma16(o[u][4 * h + 2 * t], p[u][i], w[t][0], w[t][1]);
+              mma16(o[u][4 * h + 2 * t + 1], p[u][i], w[t][2], w[t][3]);
+            }
+        }
     }
     if (tile + 1 < tiles) store(buf ^ 1);                                      // (the tile before this one has been read by all: the barrier below)
     __syncthreads();
   }
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-    if (g + 8 * r >= rows) continue;
-    const int64_t row = first + g + 8 * r, token = row / a.group, h = (int64_t)head * a.group + row - token * a.group;
-    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-    __nv_bfloat16* const to = a.out + (e.first + token) * a.ld_out + h * c.dim;
+  for (int u = 0; u < MT; ++u)
 #pragma unroll
-    for (int t = 0; t < kOut; ++t)
-      if (8 * t < c.dim) *reinterpret_cast<uint32_t*>(to + 8 * t + 2 * cc) = pack_bf16x2(o[t][2 * r] * inv, o[t][2 * r + 1] * inv);
-    if (cc == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = l[r] == 0.f ? -INFINITY : (log2f(l[r]) + (m[r] - 14.f)) * 0.69314718f;
-  }
+    for (int r = 0; r < 2; ++r) {
+      float sum = l[u][r];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      const int in_warp = 16 * u + 8 * r + g;
+      if (in_warp >= rows) continue;
+      const int64_t row = first + in_warp, token = row / a.group, h = (int64_t)head * a.group + row - token * a.group;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      __nv_bfloat16* const to = a.out + (e.first + token) * a.ld_out + h * c.dim;
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+        if (8 * t < c.dim) *reinterpret_cast<uint32_t*>(to + 8 * t + 2 * cc) = pack_bf16x2(o[u][t][2 * r] * inv, o[u][t][2 * r + 1] * inv);
+      if (cc == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (m[u][r] - 14.f)) * 0.69314718f;
+    }
 }
 
 constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + 255) / 256 * 256; }
@@ -674,30 +689,31 @@ qm_status launch_rows(RowsArgs a, cudaStream_t s) {
   }
   return QM_OK;
 }
-template <int FMT, int DIM>
+template <int FMT, int DIM, int MT>
 qm_status launch_tiles(const RowsArgs& a, cudaStream_t s) {
-  constexpr auto kern = attention_tiles<FMT, DIM>;
+  constexpr auto kern = attention_tiles<FMT, DIM, MT>;
   static std::atomic<bool> ready[kMaxDevices];
   const int dev = current_device();
   if (dev < 0) return QM_ERR_UNSUPPORTED;
   if (!ready[dev].load(std::memory_order_relaxed)) {
-    QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(2 * tile_bytes<DIM>())));
+    QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tiles_smem<DIM>(MT)));
     ready[dev].store(true, std::memory_order_relaxed);
   }
-  const int64_t candidates = a.c.tokens * a.group / kTileRows + a.c.batch;
-  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)candidates, (unsigned)a.c.kv_heads), dim3(256), 2 * tile_bytes<DIM>(), s, a, candidates));
+  const int64_t candidates = a.c.tokens * a.group / (128 * MT) + a.c.batch;
+  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)candidates, (unsigned)a.c.kv_heads), dim3(256), tiles_smem<DIM>(MT), s, a, candidates));
   count_launch();
   return QM_OK;
 }
 
 // Which sequences are whose: attention_tiles takes those with 64 query rows of a cached head or more, if the call has enough of them to give a third
-// of the SMs 128 rows; its thread blocks do not share keys, attention_rows does, whatever the rows.
+// of the SMs 128 rows; its thread blocks do not share keys, attention_rows does, whatever the rows.  256 rows to a thread block where there are enough for all SMs.
 template <int FMT, int DIM>
 qm_status launch_both(RowsArgs a, cudaStream_t s) {
-  const bool tiles = (a.c.tokens - a.c.batch + 1) * a.group >= 64 && a.c.tokens * a.group / kTileRows * a.c.kv_heads >= sm_count() / 3 && a.c.kv_heads < 65536;
+  const int64_t blocks = a.c.tokens * a.group / 128 * a.c.kv_heads;
+  const bool tiles = (a.c.tokens - a.c.batch + 1) * a.group >= 64 && blocks >= sm_count() / 3 && a.c.kv_heads < 65536;
   a.most_rows = tiles ? 64 : 0x7fffffff;
   if (tiles) {
-    const qm_status st = launch_tiles<FMT, DIM>(a, s);
+    const qm_status st = blocks >= 2 * sm_count() ? launch_tiles<FMT, DIM, 2>(a, s) : launch_tiles<FMT, DIM, 1>(a, s);
     if (st != QM_OK) return st;
   }
   return launch_rows<FMT, DIM>(a, s);
