@@ -42,6 +42,7 @@ struct RowsArgs {
 struct Share { int64_t lo, start, end; int b, item; };
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -195,36 +196,60 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
       };
       auto base_of = [&](int cell, int i, int page) {
         const int token = cell * kCell + 16 * i;
-        return (((int64_t)page * c.kv_heads + head << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim;
+        return ((((int64_t)page * c.kv_heads + head) << c.shift) + (token & ((1 << c.shift) - 1))) * c.dim;
       };
+      // A cell that all rows see, of a head that fills the registers' places, is loaded without a condition or an offset to be computed.
+      const bool fits = c.dim == DIM;
       auto load_k = [&](int cell, const int (&p)[2]) {
+        if (fits && p[0] >= 0 && p[1] >= 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int64_t base = base_of(cell, i, p[i]);
+          for (int i = 0; i < 2; ++i) {
+            const uint8_t* const from = c.k + base_of(cell, i, p[i]) + g * DIM + cc * 16;
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int h = 0; h < kChunks; ++h) {
-              const int d = (cc + 4 * h) * 16;
-              k[2 * i + t][h] = p[i] >= 0 && d < c.dim ? load_words(c.k + base + (8 * t + g) * c.dim + d, Words<4>()) : Words<4>{};
-            }
-          // (a page that the table does not have, or has wrong: NaN for whoever sees its tokens)
-          dk[i] = p[i] >= 0 ? __ldg(c.dk + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+              for (int h = 0; h < kChunks; ++h) k[2 * i + t][h] = load_words(from + 8 * t * DIM + 64 * h, Words<4>());
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int64_t base = base_of(cell, i, max(p[i], 0));
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int h = 0; h < kChunks; ++h) {
+                const int d = (cc + 4 * h) * 16;
+                k[2 * i + t][h] = p[i] >= 0 && d < c.dim ? load_words(c.k + base + (8 * t + g) * c.dim + d, Words<4>()) : Words<4>{};
+              }
+          }
         }
+        // (a page that the table does not have, or has wrong: NaN for whoever sees its tokens)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) dk[i] = p[i] >= 0 ? __ldg(c.dk + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
       };
       auto load_v = [&](int cell, const int (&p)[2]) {
+        if (fits && p[0] >= 0 && p[1] >= 0 && (cell + 1) * kCell <= most) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int64_t base = base_of(cell, i, p[i]);
+          for (int i = 0; i < 2; ++i) {
+            const uint8_t* const from = c.v + base_of(cell, i, p[i]) + 2 * cc * DIM + g * 4 * kWide;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int token = 2 * cc + (t & 1) + 8 * (t >> 1), d = g * 4 * kWide;
-            // (nothing of what lies behind the last key that is seen: its codes may be anything, and 0 times NaN is not 0)
-            v[i][t] = p[i] >= 0 && d < c.dim && cell * kCell + 16 * i + token < most ? load_words(c.v + base + token * c.dim + d, Words<kWide>())
-                                                                                    : Words<kWide>{};
+            for (int t = 0; t < 4; ++t) v[i][t] = load_words(from + ((t & 1) + 8 * (t >> 1)) * DIM, Words<kWide>());
           }
-          dv[i] = p[i] >= 0 ? __ldg(c.dv + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int64_t base = base_of(cell, i, max(p[i], 0));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const int token = 2 * cc + (t & 1) + 8 * (t >> 1), d = g * 4 * kWide;
+              // (nothing of what lies behind the last key that is seen: its codes may be anything, and 0 times NaN is not 0)
+              v[i][t] = p[i] >= 0 && d < c.dim && cell * kCell + 16 * i + token < most ? load_words(c.v + base + token * c.dim + d, Words<kWide>())
+                                                                                      : Words<kWide>{};
+            }
+          }
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) dv[i] = p[i] >= 0 ? __ldg(c.dv + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
       };
       int here[2], next[2];
       int cell = cell0 + warp;
@@ -257,18 +282,23 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
         for (int i = 0; i < 2; ++i) {
           const bool tiny = cv[i] < kLeastScale;
           weigh[i] = tiny ? -60.f : lg2(cv[i]);
-          inverse[i] = tiny ? 1.1529215e18f : __frcp_rn(cv[i]);
+          inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
         }
-        const bool partial = (cell + 1) * kCell > least;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = i >> 1;
-            s[t][i] = fmaf(s[t][i], factor[r] * ck[t >> 1], weigh[t >> 1]);
-            if (partial && cell * kCell + 8 * t + 2 * cc + (i & 1) >= limit[r]) s[t][i] = -INFINITY;
-            top[r] = fmaxf(top[r], s[t][i]);
-          }
+          for (int i = 0; i < 4; ++i) s[t][i] = fmaf(s[t][i], factor[i >> 1] * ck[t >> 1], weigh[t >> 1]);
+        if ((cell + 1) * kCell > least) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (cell * kCell + 8 * t + 2 * cc + (i & 1) >= limit[i >> 1]) s[t][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[t][i]);
         float from[2];
         bool moved = false;
 #pragma unroll
@@ -577,7 +607,7 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
         cv[i] = scales[buf][1][i];
         const bool tiny = cv[i] < kLeastScale;
         weigh[i] = tiny ? -60.f : lg2(cv[i]);
-        inverse[i] = tiny ? 1.1529215e18f : __frcp_rn(cv[i]);
+        inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
       }
       const bool partial = (tile + 1) * kTileKeys > least;
       uint32_t p[MT][kGroups][4];
@@ -588,13 +618,19 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
         for (int t = 0; t < 2 * kGroups; ++t) {
           const float ck = scales[buf][0][t >> 1];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = i >> 1;
-            s[u][t][i] = fmaf(s[u][t][i], factor[u][r] * ck, weigh[t >> 1]);
-            if (partial && tile * kTileKeys + 8 * t + 2 * cc + (i & 1) >= limit[u][r]) s[u][t][i] = -INFINITY;
-            top[r] = fmaxf(top[r], s[u][t][i]);
-          }
+          for (int i = 0; i < 4; ++i) s[u][t][i] = fmaf(s[u][t][i], factor[u][i >> 1] * ck, weigh[t >> 1]);
         }
+        if (partial) {
+#pragma unroll
+          for (int t = 0; t < 2 * kGroups; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (tile * kTileKeys + 8 * t + 2 * cc + (i & 1) >= limit[u][i >> 1]) s[u][t][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * kGroups; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[u][t][i]);
         bool moved = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
