@@ -10,7 +10,7 @@
 //
 // attention_rows: 16 query rows (tokens x query heads of one cached head) at a time against all keys, mma.sync m16n8k16 from registers: a
 // thread loads 16 bytes of keys or values straight from the cache in the places that the instruction's operands have, so nothing goes through
-// shared memory. A thread block takes an equal share of the cells (32 tokens for 16 rows and a head) of all sequences together, wherever they begin
+// shared memory. A thread block takes an equal share of the cells (32 or 16 tokens for 16 rows and a head) of all sequences together, wherever they begin
 // and end; what is left of rows whose keys were shared out is joined by attention_join, in the order of the keys.
 //
 // attention_tiles, for sequences with many query rows: 128 or 256 of them to a thread block. Tiles of 32 keys and values are turned into fp16
@@ -23,7 +23,7 @@
 namespace qm {
 namespace {
 
-constexpr int kWarps = 8, kRows = 16, kCell = 32;
+constexpr int kWarps = 8, kRows = 16;
 constexpr int kMaxBlocks = 512;                 // of a launch
 
 struct RowsArgs {
@@ -73,16 +73,20 @@ __device__ __forceinline__ Words<2> load_words(const uint8_t* p, Words<2>) {
   return r;
 }
 
-__device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e) {
+// Tokens of a cell: what a warp has of keys and values at a time and on their way, 4 KB.
+__host__ __device__ constexpr int cell_of(int dim) { return dim == 64 ? 32 : 16; }
+__device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e, int kCell) {
   if (e.n == 0 || (int64_t)e.n * a.group >= a.most_rows) return 0;
   return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.len + kCell - 1) / kCell);
 }
 
 template <int FMT, int DIM>
-__global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows(const RowsArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs a) {
   constexpr int kChunks = DIM / 64;              // 16-byte pieces of a key in a thread
   constexpr int kWide = DIM / 32;                // words of a value in a thread
   constexpr int kTiles = DIM / 8;                // output tiles of eight dims
+  constexpr int kCell = cell_of(DIM), kN = kCell / 16;
+  __shared__ uint4 queries[4 * kChunks][32];     // as the products' left operands
   __shared__ int64_t sums[kWarps];
   __shared__ int64_t found_lo;
   __shared__ int found_b;
@@ -95,7 +99,7 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
   // ---- this thread block's share: all cells in one line, sequence by sequence, head by head, rows by rows
   auto scan = [&](int base, int64_t& mine) {     // this thread's sequence's cells; the sum up to and with it
     const int b = base + tid;
-    mine = b < c.batch ? cells_of(a, extent_of(c, b)) : 0;
+    mine = b < c.batch ? cells_of(a, extent_of(c, b), kCell) : 0;
     int64_t up = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += t; }
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
   bool first = true;
   for (int64_t pos = lo; pos < hi; ++b) {
     const Extent e = extent_of(c, b);
-    const int64_t mine_all = cells_of(a, e);
+    const int64_t mine_all = cells_of(a, e, kCell);
     if (mine_all == 0) continue;
     const int per = max(1, (e.len + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
     for (int item = (int)((pos - at) / per); pos < hi && item < c.kv_heads * tiles; ++item) {
@@ -148,9 +152,9 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
       const int cell0 = (int)(pos - start), quota = hi < end ? (int)(hi - start) : per, cell1 = min(quota, (most + kCell - 1) / kCell);
 
       // ---- queries: rows g and g + 8, in the order of dims in which a thread has its part of a key
-      uint32_t q[4 * kChunks][4];
       float factor[2];
       {
+        uint32_t q[4 * kChunks][4];
         const __nv_bfloat16* from[2];
         float top[2] = {0.f, 0.f};
         uint2 raw[2][4 * kChunks];
@@ -175,6 +179,13 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
             q[s][2 + r] = pack_half2(bf16_lo(raw[r][s].y) * by, bf16_hi(raw[r][s].y) * by);
           }
         }
+        // (the barriers: the last rows' queries have been read by all; these are there)
+        __syncthreads();
+        if (warp < 4 * kChunks)
+#pragma unroll
+          for (int s = 0; s < 4 * kChunks; ++s)
+            if (s == warp) queries[s][lane] = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
+        __syncthreads();
       }
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
       float o[kTiles][4];
@@ -183,13 +194,13 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
 
-      // ---- cells: keys and values of 32 tokens, the next cell's on their way
-      Words<4> k[4][kChunks];
-      Words<kWide> v[2][4];
-      float dk[2], dv[2];
-      auto pages = [&](int cell, int (&p)[2]) {
+      // ---- cells: their keys and values in registers, the next cell's on their way
+      Words<4> k[2 * kN][kChunks];
+      Words<kWide> v[kN][4];
+      float dk[kN], dv[kN];
+      auto pages = [&](int cell, int (&p)[kN]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kN; ++i) {
           const int token = cell * kCell + 16 * i;
           p[i] = cell < cell1 && token < most ? page_of(c, b, token >> c.shift) : -1;
         }
@@ -200,10 +211,10 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
       };
       // A cell that all rows see, of a head that fills the registers' places, is loaded without a condition or an offset to be computed.
       const bool fits = c.dim == DIM;
-      auto load_k = [&](int cell, const int (&p)[2]) {
-        if (fits && p[0] >= 0 && p[1] >= 0) {
+      auto load_k = [&](int cell, const int (&p)[kN]) {
+        if (fits && p[0] >= 0 && p[kN - 1] >= 0) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < kN; ++i) {
             const uint8_t* const from = c.k + base_of(cell, i, p[i]) + g * DIM + cc * 16;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -212,7 +223,7 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < kN; ++i) {
             const int64_t base = base_of(cell, i, max(p[i], 0));
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -225,19 +236,19 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
         }
         // (a page that the table does not have, or has wrong: NaN for whoever sees its tokens)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) dk[i] = p[i] >= 0 ? __ldg(c.dk + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+        for (int i = 0; i < kN; ++i) dk[i] = p[i] >= 0 ? __ldg(c.dk + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
       };
-      auto load_v = [&](int cell, const int (&p)[2]) {
-        if (fits && p[0] >= 0 && p[1] >= 0 && (cell + 1) * kCell <= most) {
+      auto load_v = [&](int cell, const int (&p)[kN]) {
+        if (fits && p[0] >= 0 && p[kN - 1] >= 0 && (cell + 1) * kCell <= most) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < kN; ++i) {
             const uint8_t* const from = c.v + base_of(cell, i, p[i]) + 2 * cc * DIM + g * 4 * kWide;
 #pragma unroll
             for (int t = 0; t < 4; ++t) v[i][t] = load_words(from + ((t & 1) + 8 * (t >> 1)) * DIM, Words<kWide>());
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < kN; ++i) {
             const int64_t base = base_of(cell, i, max(p[i], 0));
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -249,54 +260,60 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
           }
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) dv[i] = p[i] >= 0 ? __ldg(c.dv + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
+        for (int i = 0; i < kN; ++i) dv[i] = p[i] >= 0 ? __ldg(c.dv + (int64_t)p[i] * c.kv_heads + head) : __int_as_float(0x7fffffff);
       };
-      int here[2], next[2];
+      int here[kN], next[kN];
       int cell = cell0 + warp;
       pages(cell, here);
       if (cell < cell1) { load_k(cell, here); load_v(cell, here); }
       pages(cell + kWarps, next);
       for (; cell < cell1; cell += kWarps) {
         // scores
-        float s[4][4];
+        float s[2 * kN][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 2 * kN; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
 #pragma unroll
-          for (int h = 0; h < kChunks; ++h)
+        for (int h = 0; h < kChunks; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 4; ++j) {
+            const uint4 w = queries[4 * h + j][lane];
+            const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int t = 0; t < 2 * kN; ++t) {
               uint32_t b0, b1;
               half4_of<FMT>(k[t][h].w[j], b0, b1);
-              mma16(s[t], q[4 * h + j], b0, b1);
+              mma16(s[t], q, b0, b1);
             }
-        }
-        const float ck[2] = {dk[0], dk[1]}, cv[2] = {dv[0], dv[1]};
+          }
+        float ck[kN], cv[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) { ck[i] = dk[i]; cv[i] = dv[i]; }
         const bool more = cell + kWarps < cell1;
         if (more) load_k(cell + kWarps, next);
         // to the base 2, with the values' scales, masked
         float top[2] = {m[0], m[1]};
-        float weigh[2], inverse[2];
+        float weigh[kN], inverse[kN];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kN; ++i) {
           const bool tiny = cv[i] < kLeastScale;
           weigh[i] = tiny ? -60.f : lg2(cv[i]);
           inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 2 * kN; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[t][i] = fmaf(s[t][i], factor[i >> 1] * ck[t >> 1], weigh[t >> 1]);
         if ((cell + 1) * kCell > least) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+          for (int t = 0; t < 2 * kN; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (cell * kCell + 8 * t + 2 * cc + (i & 1) >= limit[i >> 1]) s[t][i] = -INFINITY;
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 2 * kN; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[t][i]);
         float from[2];
@@ -320,9 +337,9 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
 #pragma unroll
         for (int r = 0; r < 2; ++r) from[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
         // weights, in the places of a left operand
-        uint32_t p[2][4];
+        uint32_t p[kN][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kN; ++i)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             float e0 = ex2(s[2 * i][2 * r] - from[r]), e1 = ex2(s[2 * i][2 * r + 1] - from[r]);
@@ -334,7 +351,7 @@ __global__ void __launch_bounds__(kWarps * 32, DIM == 64 ? 2 : 1) attention_rows
             p[i][2 + r] = none ? 0u : pack_half2(e2, e3);
           }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kN; ++i)
 #pragma unroll
           for (int w = 0; w < kWide; ++w) {
             uint32_t b[4][2];
