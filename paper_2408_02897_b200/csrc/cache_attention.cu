@@ -23,7 +23,7 @@
 namespace qm {
 namespace {
 
-constexpr int kWarps = 8, kRows = 16;
+constexpr int kWarps = 8, kMostRows = 16;
 constexpr int kMaxBlocks = 512;                 // of a launch
 
 struct RowsArgs {
@@ -33,6 +33,7 @@ struct RowsArgs {
   float scale_log2;                              // of scores to the base 2
   __nv_bfloat16* out; int64_t ld_out;
   float* lse;
+  int rows;                                      // to a cell of attention_rows, 8 or 16
   int most_rows;                                 // sequences with as many query rows of a cached head or more are attention_tiles'
   struct Share* shares;                          // one a thread block
   float* parts;                                  // [2 * blocks][16][padded dim + 2]
@@ -73,20 +74,28 @@ __device__ __forceinline__ Words<2> load_words(const uint8_t* p, Words<2>) {
   return r;
 }
 
-// Tokens of a cell: what a warp has of keys and values at a time and on their way, 4 KB.
-__host__ __device__ constexpr int cell_of(int dim) { return dim == 64 ? 32 : 16; }
-__device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e, int kCell) {
+// Tokens of a cell, whose keys and values a warp has in registers or on their way there.
+__host__ __device__ constexpr int cell_of(int dim, bool narrow) { return narrow || dim == 64 ? 32 : 16; }
+__device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e, int kRows, int kCell) {
   if (e.n == 0 || (int64_t)e.n * a.group >= a.most_rows) return 0;
   return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.len + kCell - 1) / kCell);
 }
 
-template <int FMT, int DIM>
+__device__ __forceinline__ uint32_t turned(uint32_t x) {            // 8x8 of 16 bits, a row to four lanes
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+// NARROW: eight query rows instead of 16, as the products' N: keys and values are their left operands then, and half as many products, exponentials
+// and sums make a cell. A token at a time with up to eight query heads to a cached one leaves the wider form's rows empty (64 tokens on 8192 172 us).
+template <int FMT, int DIM, bool NARROW>
 __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs a) {
   constexpr int kChunks = DIM / 64;              // 16-byte pieces of a key in a thread
   constexpr int kWide = DIM / 32;                // words of a value in a thread
   constexpr int kTiles = DIM / 8;                // output tiles of eight dims
-  constexpr int kCell = cell_of(DIM), kN = kCell / 16;
-  __shared__ uint4 queries[4 * kChunks][32];     // as the products' left operands
+  constexpr int kCell = cell_of(DIM, NARROW), kN = kCell / 16, kRows = NARROW ? 8 : 16, kSums = NARROW ? kTiles / 2 : kTiles;
+  __shared__ uint4 queries[4 * kChunks][32];     // as the products' operands
   __shared__ int64_t sums[kWarps];
   __shared__ int64_t found_lo;
   __shared__ int found_b;
@@ -99,7 +108,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
   // ---- this thread block's share: all cells in one line, sequence by sequence, head by head, rows by rows
   auto scan = [&](int base, int64_t& mine) {     // this thread's sequence's cells; the sum up to and with it
     const int b = base + tid;
-    mine = b < c.batch ? cells_of(a, extent_of(c, b), kCell) : 0;
+    mine = b < c.batch ? cells_of(a, extent_of(c, b), kRows, kCell) : 0;
     int64_t up = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += t; }
@@ -136,7 +145,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
   bool first = true;
   for (int64_t pos = lo; pos < hi; ++b) {
     const Extent e = extent_of(c, b);
-    const int64_t mine_all = cells_of(a, e, kCell);
+    const int64_t mine_all = cells_of(a, e, kRows, kCell);
     if (mine_all == 0) continue;
     const int per = max(1, (e.len + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
     for (int item = (int)((pos - at) / per); pos < hi && item < c.kv_heads * tiles; ++item) {
@@ -146,51 +155,54 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
       const int rows = min(kRows, e.n * a.group - row0);
       // keys up to the position of the row's token; a token whose position is below 0 sees none
       auto limit_of = [&](int r) { return r < rows ? max(0, e.len - e.n + (row0 + r) / a.group + 1) : 0; };
-      const int limit[2] = {limit_of(g), limit_of(g + 8)};
+      const int limit[2] = {limit_of(NARROW ? 2 * cc : g), limit_of(NARROW ? 2 * cc + 1 : g + 8)};      // of the rows whose statistics this thread has
       const int least = limit_of(0), most = limit_of(rows - 1);
       // (a 64-bit min(end, hi) in place of the choice was compiled to per in all but a share's first rows: nvcc 12.9)
       const int cell0 = (int)(pos - start), quota = hi < end ? (int)(hi - start) : per, cell1 = min(quota, (most + kCell - 1) / kCell);
 
-      // ---- queries: rows g and g + 8, in the order of dims in which a thread has its part of a key
+      // ---- queries: row g, or rows g and g + 8, in the order of dims in which a thread has its part of a key
       float factor[2];
       {
-        uint32_t q[4 * kChunks][4];
-        const __nv_bfloat16* from[2];
-        float top[2] = {0.f, 0.f};
-        uint2 raw[2][4 * kChunks];
+        constexpr int kR = NARROW ? 1 : 2;
+        uint32_t q[4 * kChunks][4] = {};
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < kR; ++r) {
+          float top = 0.f;
+          uint2 raw[4 * kChunks];
           const int row = row0 + g + 8 * r, token = row / a.group;
-          from[r] = a.q + (e.first + token) * a.ld_q + ((int64_t)head * a.group + row - token * a.group) * c.dim;
+          const __nv_bfloat16* const from = a.q + (e.first + token) * a.ld_q + ((int64_t)head * a.group + row - token * a.group) * c.dim;
 #pragma unroll
           for (int s = 0; s < 4 * kChunks; ++s) {
             const int d = (cc + 4 * (s >> 2)) * 16 + 4 * (s & 3);
-            raw[r][s] = g + 8 * r < rows && d < c.dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0u, 0u);
-            top[r] = fmaxf(top[r], fmaxf(fmaxf(fabsf(bf16_lo(raw[r][s].x)), fabsf(bf16_hi(raw[r][s].x))),
-                                         fmaxf(fabsf(bf16_lo(raw[r][s].y)), fabsf(bf16_hi(raw[r][s].y)))));
+            raw[s] = g + 8 * r < rows && d < c.dim ? *reinterpret_cast<const uint2*>(from + d) : make_uint2(0u, 0u);
+            top = fmaxf(top, fmaxf(fmaxf(fabsf(bf16_lo(raw[s].x)), fabsf(bf16_hi(raw[s].x))), fmaxf(fabsf(bf16_lo(raw[s].y)), fabsf(bf16_hi(raw[s].y)))));
           }
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-          const float by = row_scale(top[r]);
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const float by = row_scale(top);
           factor[r] = a.scale_log2 / by;
 #pragma unroll
           for (int s = 0; s < 4 * kChunks; ++s) {
-            q[s][r] = pack_half2(bf16_lo(raw[r][s].x) * by, bf16_hi(raw[r][s].x) * by);
-            q[s][2 + r] = pack_half2(bf16_lo(raw[r][s].y) * by, bf16_hi(raw[r][s].y) * by);
+            q[s][r] = pack_half2(bf16_lo(raw[s].x) * by, bf16_hi(raw[s].x) * by);
+            q[s][2 + r] = pack_half2(bf16_lo(raw[s].y) * by, bf16_hi(raw[s].y) * by);
           }
+        }
+        if (NARROW) {
+          const float mine = factor[0];
+          factor[0] = __shfl_sync(0xffffffffu, mine, 8 * cc);
+          factor[1] = __shfl_sync(0xffffffffu, mine, 8 * cc + 4);
         }
         // (the barriers: the last rows' queries have been read by all; these are there)
         __syncthreads();
-        if (warp < 4 * kChunks)
 #pragma unroll
-          for (int s = 0; s < 4 * kChunks; ++s)
-            if (s == warp) queries[s][lane] = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
+        for (int s = 0; s < 4 * kChunks; ++s)
+          if (s == warp) queries[s][lane] = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
         __syncthreads();
       }
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-      float o[kTiles][4];
+      float o[kSums][4];
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+      for (int t = 0; t < kSums; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
 
@@ -268,10 +280,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
       if (cell < cell1) { load_k(cell, here); load_v(cell, here); }
       pages(cell + kWarps, next);
       for (; cell < cell1; cell += kWarps) {
-        // scores
-        float s[2 * kN][4];
+        // scores: s[t][i] of row i / 2 (g or g + 8) and key 8 t + 2 cc + i % 2, or narrow of row 2 cc + i % 2 and key 16 t + g + 8 (i / 2)
+        constexpr int kS = NARROW ? kN : 2 * kN;
+        float s[kS][4];
 #pragma unroll
-        for (int t = 0; t < 2 * kN; ++t)
+        for (int t = 0; t < kS; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[t][i] = 0.f;
 #pragma unroll
@@ -281,10 +294,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
             const uint4 w = queries[4 * h + j][lane];
             const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int t = 0; t < 2 * kN; ++t) {
-              uint32_t b0, b1;
-              half4_of<FMT>(k[t][h].w[j], b0, b1);
-              mma16(s[t], q, b0, b1);
+            for (int t = 0; t < kN; ++t) {
+              uint32_t x[4];
+              half4_of<FMT>(k[2 * t][h].w[j], x[0], x[2]);
+              half4_of<FMT>(k[2 * t + 1][h].w[j], x[1], x[3]);
+              if (NARROW) mma16(s[t], x, q[0], q[2]);
+              else {
+                mma16(s[NARROW ? 0 : 2 * t], q, x[0], x[2]);
+                mma16(s[NARROW ? 0 : 2 * t + 1], q, x[1], x[3]);
+              }
             }
           }
         float ck[kN], cv[kN];
@@ -302,26 +320,34 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
           inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
         }
 #pragma unroll
-        for (int t = 0; t < 2 * kN; ++t)
+        for (int t = 0; t < kS; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][i] = fmaf(s[t][i], factor[i >> 1] * ck[t >> 1], weigh[t >> 1]);
+          for (int i = 0; i < 4; ++i) {
+            const int r = NARROW ? i & 1 : i >> 1, n = NARROW ? t : t >> 1;
+            s[t][i] = fmaf(s[t][i], factor[r] * ck[n], weigh[n]);
+          }
         if ((cell + 1) * kCell > least) {
 #pragma unroll
-          for (int t = 0; t < 2 * kN; ++t)
+          for (int t = 0; t < kS; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (cell * kCell + 8 * t + 2 * cc + (i & 1) >= limit[i >> 1]) s[t][i] = -INFINITY;
+              if (cell * kCell + (NARROW ? 16 * t + g + 8 * (i >> 1) : 8 * t + 2 * cc + (i & 1)) >= limit[NARROW ? i & 1 : i >> 1]) s[t][i] = -INFINITY;
         }
 #pragma unroll
-        for (int t = 0; t < 2 * kN; ++t)
+        for (int t = 0; t < kS; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[t][i]);
+          for (int i = 0; i < 4; ++i) top[NARROW ? i & 1 : i >> 1] = fmaxf(top[NARROW ? i & 1 : i >> 1], s[t][i]);
         float from[2];
         bool moved = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          if (NARROW) {
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], x));
+          } else {
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          }
           moved |= top[r] > m[r];
         }
         if (__any_sync(0xffffffffu, moved)) {
@@ -331,25 +357,38 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
             m[r] = top[r];
             l[r] *= shrink;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) { o[t][2 * r] *= shrink; o[t][2 * r + 1] *= shrink; }
+            for (int t = 0; t < kSums; ++t) {
+              o[t][NARROW ? r : 2 * r] *= shrink;
+              o[t][NARROW ? 2 + r : 2 * r + 1] *= shrink;
+            }
           }
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r) from[r] = m[r] == -INFINITY ? 0.f : m[r] - 14.f;
-        // weights, in the places of a left operand
+        // weights, in the places of an operand
         uint32_t p[kN][4];
 #pragma unroll
-        for (int i = 0; i < kN; ++i)
+        for (int n = 0; n < kN; ++n) {
+          const bool none = cv[n] < kLeastScale;
+          float x[2][4];                                                     // [row][key]
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            float e0 = ex2(s[2 * i][2 * r] - from[r]), e1 = ex2(s[2 * i][2 * r + 1] - from[r]);
-            float e2 = ex2(s[2 * i + 1][2 * r] - from[r]), e3 = ex2(s[2 * i + 1][2 * r + 1] - from[r]);
-            const float sum = (e0 + e1) + (e2 + e3);
-            if (sum != 0.f) l[r] = fmaf(sum, inverse[i], l[r]);         // (nothing of a block that the row does not see, whatever its scale)
-            const bool none = cv[i] < kLeastScale;
-            p[i][r] = none ? 0u : pack_half2(e0, e1);
-            p[i][2 + r] = none ? 0u : pack_half2(e2, e3);
+#pragma unroll
+            for (int i = 0; i < (NARROW ? 2 : 4); ++i) x[r][i] = ex2((NARROW ? s[n][2 * i + r] : s[NARROW ? 0 : 2 * n + (i >> 1)][2 * r + (i & 1)]) - from[r]);
+            const float sum = NARROW ? x[r][0] + x[r][1] : (x[r][0] + x[r][1]) + (x[r][2] + x[r][3]);
+            if (sum != 0.f) l[r] = fmaf(sum, inverse[n], l[r]);               // (nothing of a block that the row does not see, whatever its scale)
           }
+          if (NARROW) {
+            p[n][0] = turned(none ? 0u : pack_half2(x[0][0], x[1][0]));
+            p[n][1] = turned(none ? 0u : pack_half2(x[0][1], x[1][1]));
+          } else {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              p[n][r] = none ? 0u : pack_half2(x[r][0], x[r][1]);
+              p[n][2 + r] = none ? 0u : pack_half2(x[r][2], x[r][3]);
+            }
+          }
+        }
 #pragma unroll
         for (int i = 0; i < kN; ++i)
 #pragma unroll
@@ -361,8 +400,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
               half4_of<FMT>(__byte_perm(x, y, 0x5140), b[0][h], b[1][h]);
               half4_of<FMT>(__byte_perm(x, y, 0x7362), b[2][h], b[3][h]);
             }
+            if (NARROW) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma16(o[4 * w + j], p[i], b[j][0], b[j][1]);
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t x[4] = {b[2 * j][0], b[2 * j + 1][0], b[2 * j][1], b[2 * j + 1][1]};
+                mma16(o[2 * w + j], x, p[i][0], p[i][1]);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma16(o[NARROW ? 0 : 4 * w + j], p[i], b[j][0], b[j][1]);
+            }
           }
         if (more) {
           load_v(cell + kWarps, next);
@@ -374,18 +421,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
       __syncthreads();                                                   // (the last rows' have been read)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        if (cc == 0) { stat_m[warp][g + 8 * r] = m[r]; stat_l[warp][g + 8 * r] = l[r]; }
-        if (g + 8 * r < rows) {
-          float* const to = joined + (warp * kRows + g + 8 * r) * (DIM + 4);
-          // tile t, column n stands for dim n * kTiles + t: a thread has columns 2 cc and 2 cc + 1
+        const int row = NARROW ? 2 * cc + r : g + 8 * r;
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+        for (int x = NARROW ? 4 : 1; x < (NARROW ? 32 : 4); x *= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], x);
+        if ((NARROW ? g : cc) == 0) { stat_m[warp][row] = m[r]; stat_l[warp][row] = l[r]; }
+        if (row < rows) {
+          float* const to = joined + (warp * kRows + row) * (DIM + 4);
+          // tile t, column n stands for dim n * kTiles + t (wide: a thread has columns 2 cc and 2 cc + 1; narrow: column g, tiles 2 t and 2 t + 1)
+          if (NARROW) {
 #pragma unroll
-            for (int t = 0; t < kTiles; t += 4)
-              *reinterpret_cast<float4*>(to + (2 * cc + h) * kTiles + t) =
-                  make_float4(o[t][2 * r + h], o[t + 1][2 * r + h], o[t + 2][2 * r + h], o[t + 3][2 * r + h]);
+            for (int t = 0; t < kSums; t += 2)
+              *reinterpret_cast<float4*>(to + g * kTiles + 2 * t) = make_float4(o[t][r], o[t][2 + r], o[t + 1][r], o[t + 1][2 + r]);
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int t = 0; t + 3 < kSums; t += 4)
+                *reinterpret_cast<float4*>(to + (2 * cc + h) * kTiles + t) =
+                    make_float4(o[t][2 * r + h], o[t + 1][2 * r + h], o[t + 2][2 * r + h], o[t + 3][2 * r + h]);
+          }
         }
       }
       __syncthreads();
@@ -412,7 +466,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
                 make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
           if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (top - 14.f)) * 0.69314718f;
         } else {
-          float* const to = a.parts + ((int64_t)slot * kRows + r) * (DIM + 2);
+          float* const to = a.parts + ((int64_t)slot * kMostRows + r) * (DIM + 2);
           to[d] = y.x; to[d + 1] = y.y; to[d + 2] = y.z; to[d + 3] = y.w;
           if (d == 0) { to[DIM] = top; to[DIM + 1] = sum; }
         }
@@ -433,13 +487,13 @@ __global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid
   if (s.lo <= s.start || s.lo >= s.end || a.shares[i - 1].lo > s.start) return;
   const CacheView& c = a.c;
   const Extent e = extent_of(c, s.b);
-  const int tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows), head = s.item / tiles, row0 = (s.item - head * tiles) * kRows;
-  const int rows = min(kRows, e.n * a.group - row0), d = threadIdx.x;
+  const int tiles = (int)(((int64_t)e.n * a.group + a.rows - 1) / a.rows), head = s.item / tiles, row0 = (s.item - head * tiles) * a.rows;
+  const int rows = min(a.rows, e.n * a.group - row0), d = threadIdx.x;
   int last = i;
   while (last + 1 < grid && a.shares[last + 1].lo < s.end) ++last;
   for (int r = blockIdx.y; r < rows; r += gridDim.y) {
     float top = -INFINITY, sum = 0.f, y = 0.f;
-    auto part = [&](int j) { return a.parts + ((int64_t)(2 * j + (j == i - 1 ? 1 : 0)) * kRows + r) * (DIM + 2); };
+    auto part = [&](int j) { return a.parts + ((int64_t)(2 * j + (j == i - 1 ? 1 : 0)) * kMostRows + r) * (DIM + 2); };
     for (int j = i - 1; j <= last; ++j) top = fmaxf(top, part(j)[DIM]);
 #pragma unroll 4
     for (int j = i - 1; j <= last; ++j) {
@@ -720,10 +774,11 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
 
 constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + 255) / 256 * 256; }
 
-template <int FMT, int DIM>
+template <int FMT, int DIM, bool NARROW>
 qm_status launch_rows(RowsArgs a, cudaStream_t s) {
-  constexpr auto kern = attention_rows<FMT, DIM>;
-  constexpr size_t smem = (size_t)kWarps * kRows * (DIM + 4) * 4;
+  constexpr auto kern = attention_rows<FMT, DIM, NARROW>;
+  constexpr size_t smem = (size_t)kWarps * (NARROW ? 8 : 16) * (DIM + 4) * 4;
+  a.rows = NARROW ? 8 : 16;
   static std::atomic<int> resident[kMaxDevices];
   const int dev = current_device();
   if (dev < 0) return QM_ERR_UNSUPPORTED;
@@ -769,14 +824,15 @@ qm_status launch_both(RowsArgs a, cudaStream_t s) {
     const qm_status st = blocks >= 2 * sm_count() ? launch_tiles<FMT, DIM, 2>(a, s) : launch_tiles<FMT, DIM, 1>(a, s);
     if (st != QM_OK) return st;
   }
-  return launch_rows<FMT, DIM>(a, s);
+  // eight rows to a cell where a sequence has no more on the average
+  return a.c.tokens * a.group <= 8ll * a.c.batch ? launch_rows<FMT, DIM, true>(a, s) : launch_rows<FMT, DIM, false>(a, s);
 }
 template <int FMT>
 qm_status launch_dim(const RowsArgs& a, cudaStream_t s) { return a.c.dim <= 64 ? launch_both<FMT, 64>(a, s) : launch_both<FMT, 128>(a, s); }
 
 }  // namespace
 
-size_t cache_attention_workspace(int dim) { return share_bytes() + (size_t)2 * kMaxBlocks * kRows * ((dim <= 64 ? 64 : 128) + 2) * 4; }
+size_t cache_attention_workspace(int dim) { return share_bytes() + (size_t)2 * kMaxBlocks * kMostRows * ((dim <= 64 ? 64 : 128) + 2) * 4; }
 
 qm_status launch_cache_attention(const CacheArgs& c, const AttentionArgs& l, cudaStream_t s) {
   RowsArgs a{};

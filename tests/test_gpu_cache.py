@@ -391,3 +391,10 @@ def test_tiles_nan_and_bad_blocks():
     sees[200 + 32:] = True
     assert np.array_equal(np.isnan(out).all(2), sees) and np.array_equal(np.isnan(out).any(2), sees)
     assert np.array_equal(out[~sees], sound[~sees])
+
+
+@pytest.mark.parametrize("fmt,dim", [("int8", 64), ("e4m3", 128), ("e5m2", 80)])
+def test_one_sequence_of_several_tokens_among_many_of_one(fmt, dim):
+    """The form for eight query rows, and a sequence that has more than one such lot."""
+    new, lens = [20] + [1] * 15 + [9], [33] + [50 * i + 1 for i in range(15)] + [700]
+    check_attention(Case(fmt, 2, dim, 32, new, lens, seed=dim).fill(lens), 4)
