@@ -192,27 +192,40 @@ linear_fp8_few(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
       // a block's scales: of x for the thread's columns, then of the weights for the warp's 32 lanes (or one for all)
       constexpr int kSlot = kCols + 32;
       float* const ring = scales + (warp - 2) * kAhead * kSlot;
-      auto fetch = [&](int kb, int slot) {
-        if (kb < kb1) {
-          const uint32_t to = smem_u32(ring + slot * kSlot + lane);
+      const float* px[(kCols + 31) / 32];
+      bool there[(kCols + 31) / 32];
 #pragma unroll
-          for (int i = 0; i < kCols; i += 32)
-            if (kCols >= 32 || lane < kCols) {
-              const bool there = c0 + i + lane < live;
-              copy4(to + i * 4, a.sc.dx + (int64_t)kb * a.M + (there ? m0 + c0 + i + lane : m0), there);
-            }
-          copy4(to + kCols * 4, a.sc.dw + (int64_t)kb * a.sc.dw_cols + wcol, true);
+      for (int i = 0; i < (kCols + 31) / 32; ++i) {
+        there[i] = c0 + 32 * i + lane < live;
+        px[i] = a.sc.dx + (int64_t)kb0 * a.M + m0 + (there[i] ? c0 + 32 * i + lane : 0);
+      }
+      const float* pw = a.sc.dw + (int64_t)kb0 * a.sc.dw_cols + wcol;
+      uint32_t put = smem_u32(ring + lane);
+      const uint32_t put_end = put + kAhead * kSlot * 4;
+      int left = kb1 - kb0;
+      // (addresses and conditions are handed on from block to block: 256 x 4096 x 4096 18.7 -> 18.0 us, where no copies at all would leave 14.7)
+      auto fetch = [&]() {
+        if (left-- > 0) {
+#pragma unroll
+          for (int i = 0; i < (kCols + 31) / 32; ++i) {
+            if (kCols >= 32 || lane < kCols) copy4(put + 128 * i, px[i], there[i]);
+            px[i] += a.M;
+          }
+          copy4(put + kCols * 4, pw, true);
+          pw += a.sc.dw_cols;
         }
         copies_commit();
+        put += kSlot * 4;
+        if (put == put_end) put -= kAhead * kSlot * 4;
       };
-      for (int d = 0; d < kAhead - 1; ++d) fetch(kb0 + d, d);
+      for (int d = 0; d < kAhead - 1; ++d) fetch();
       const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16) + c0;
       int slot = 0;
       for (int kb = kb0, g = 0; kb < kb1; ++kb, ++g) {
         const int buf = g % kBufs;
         copies_wait<kAhead - 2>();
         __syncwarp();                                                        // (and the slot that is filled next has been read by all lanes)
-        fetch(kb + kAhead - 1, slot == 0 ? kAhead - 1 : slot - 1);
+        fetch();
         const float* const dx = ring + slot * kSlot;
         const uint64_t dw = both(dx[kCols + lane]);
         slot = slot == kAhead - 1 ? 0 : slot + 1;
