@@ -81,7 +81,7 @@ __device__ __forceinline__ Words<2> load_words(const uint8_t* p, Words<2>) {
 __host__ __device__ constexpr int cell_of(int dim, bool narrow) { return narrow || dim == 64 ? 32 : 16; }
 __device__ __forceinline__ int64_t cells_of(const RowsArgs& a, const Extent& e, int kRows, int kCell) {
   if (e.n == 0 || (int64_t)e.n * a.group >= a.most_rows) return 0;
-  return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.len + kCell - 1) / kCell);
+  return (int64_t)a.c.kv_heads * (((int64_t)e.n * a.group + kRows - 1) / kRows) * max(1, (e.reach + kCell - 1) / kCell);
 }
 
 __device__ __forceinline__ uint32_t turned(uint32_t x) {            // 8x8 of 16 bits, a row to four lanes
@@ -150,14 +150,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
     const Extent e = extent_of(c, b);
     const int64_t mine_all = cells_of(a, e, kRows, kCell);
     if (mine_all == 0) continue;
-    const int per = max(1, (e.len + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
+    const int per = max(1, (e.reach + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
     for (int item = (int)((pos - at) / per); pos < hi && item < c.kv_heads * tiles; ++item) {
       const int64_t start = at + (int64_t)item * per, end = start + per;
       if (first && tid == 0) a.shares[blockIdx.x] = Share{lo, start, end, b, item};
       const int head = item / tiles, row0 = (item - head * tiles) * kRows;
       const int rows = min(kRows, e.n * a.group - row0);
       // keys up to the position of the row's token; a token whose position is below 0 sees none
-      auto limit_of = [&](int r) { return r < rows ? max(0, e.len - e.n + (row0 + r) / a.group + 1) : 0; };
+      auto limit_of = [&](int r) { return r < rows ? min(e.reach, max(0, e.len - e.n + (row0 + r) / a.group + 1)) : 0; };
       const int limit[2] = {limit_of(NARROW ? 2 * cc : g), limit_of(NARROW ? 2 * cc + 1 : g + 8)};      // of the rows whose statistics this thread has
       const int least = limit_of(0), most = limit_of(rows - 1);
       // (a 64-bit min(end, hi) in place of the choice was compiled to per in all but a share's first rows: nvcc 12.9)
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
   const int64_t row0 = (cand - from_of(b)) * kTileRows, all = (int64_t)e.n * a.group;
   if (all < a.most_rows || row0 < 0 || row0 >= all) return;
 
-  auto limit_of = [&](int64_t r) { return r < all ? max(0, e.len - e.n + (int)(r / a.group) + 1) : 0; };
+  auto limit_of = [&](int64_t r) { return r < all ? min(e.reach, max(0, e.len - e.n + (int)(r / a.group) + 1)) : 0; };
   const int64_t first = row0 + 16 * MT * warp;                                 // of this warp; may be beyond the last
   const int rows = (int)min((int64_t)16 * MT, all - first);
   int limit[MT][2];

@@ -20,13 +20,16 @@ struct CacheView {
 };
 
 // A sequence's new tokens and its length with them.  What does not fit the tensors counts as no tokens at all.
-struct Extent { int64_t first; int n, len; };
+// `reach`: the length, or one more than the table's blocks hold: a token that sees a position without a block gets NaN, however many
+// there are, so a length that makes no sense costs no time.
+struct Extent { int64_t first; int n, len, reach; };
 __device__ __forceinline__ Extent extent_of(const CacheView& c, int b) {
   Extent e;
   e.first = c.starts ? c.starts[b] : b;
   const int64_t end = c.starts ? c.starts[b + 1] : b + 1;
   e.n = e.first >= 0 && end >= e.first && end <= c.tokens ? (int)(end - e.first) : 0;
   e.len = min(max(c.lens[b], 0), 0x7fff0000);       // (what is added to it stays inside 32 bits)
+  e.reach = (int)min((int64_t)e.len, ((int64_t)c.table_width << c.shift) + 1);
   return e;
 }
 

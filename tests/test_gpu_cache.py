@@ -398,3 +398,21 @@ def test_one_sequence_of_several_tokens_among_many_of_one(fmt, dim):
     """The form for eight query rows, and a sequence that has more than one such lot."""
     new, lens = [20] + [1] * 15 + [9], [33] + [50 * i + 1 for i in range(15)] + [700]
     check_attention(Case(fmt, 2, dim, 32, new, lens, seed=dim).fill(lens), 4)
+
+
+@pytest.mark.parametrize("tokens,kv", [(3, 2), (128, 32)])           # both kernels
+def test_lengths_beyond_the_table(tokens, kv):
+    """A table of three blocks and a sequence far longer: NaN for whoever sees past it, what is within it as ever, and no time spent on the rest."""
+    case = Case("int8", kv, 64, 16, [tokens, 1], [48, 40], seed=1, width=3)
+    case.tables[0] = range(3)
+    case.tables[1] = range(3, 6)
+    d = case.fill([48, 40]).device()
+    d["lens"][0] = 2 ** 30
+    q = torch.randn(tokens + 1, kv, 64, device="cuda").bfloat16()
+    out, _ = qm.qm_cache_attention(q, **d)
+    assert torch.isnan(out[:tokens]).all() and torch.isfinite(out[tokens]).all()
+    # tokens at positions 40 .. : the first eight see nothing but the table's 48
+    d["lens"][0] = 40 + tokens
+    out, _ = qm.qm_cache_attention(q, **d)
+    inside = min(tokens, 8)
+    assert torch.isfinite(out[:inside]).all() and torch.isnan(out[inside:tokens]).all() and torch.isfinite(out[tokens]).all()
