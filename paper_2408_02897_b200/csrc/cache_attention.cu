@@ -36,18 +36,33 @@ struct RowsArgs {
   float scale_log2;                              // of scores to the base 2
   __nv_bfloat16* out; int64_t ld_out;
   float* lse;
-  int rows;                                      // to a cell of attention_rows, 8 or 16
+  int rows, cell;                                // to a cell of attention_rows, 8 or 16, and its tokens
   int most_rows;                                 // sequences with as many query rows of a cached head or more are attention_tiles'
   struct Share* shares;                          // one a thread block
+  int* tiles_again;                              // whether some row of attention_tiles may have lost too much
   float* parts;                                  // [2 * blocks][16][padded dim + 2]
 };
 
-// Where a thread block's share of the cells begins, and the rows that it begins in.
-struct Share { int64_t lo, start, end; int b, item; };
+// A thread block's share of the cells, and the rows that it begins in. again: whether rows that it had all of may have lost too much (see kFewLost).
+struct Share { int64_t lo, hi, start, end; int b, item, again, pad; };
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// Blocks' scales may lie far apart, and both sums are relative to one maximum that has dv in it, which a denominator's terms may be far above or
+// below. 2^16 / dv is what they are multiplied with: for dv from 2^-61 to 2^128 that, and the sums from a weight of 1 to 2^31 of them, are normal numbers
+// (2^-112 .. 2^77, 2^-98 .. 2^122). weigh_of: log2 dv, of what counts as 0 less than any other's.
+constexpr float kDenominators = 65536.f, kLogDenominators = 16.f, kNoValues = -60.5f;
+__device__ __forceinline__ float weigh_of(float dv) { return dv < kLeastScale ? -61.f : lg2(dv); }
+// What fp32 cannot hold on the way to a denominator: the factor 2^d, d <= 0, of a new maximum is 0 below 2^-126, and a weight below 2^-140 of the
+// largest one. With log2 dv at least -61, terms so lost are below 2^(M - 65) each. The sum itself is 2^M over the largest of p dv, p a row's softmax (2^30 of
+// it in these units): where that is at most 2^16, n terms lost are below n 2^-49 of the sum. Rows where it is more are done again by attention_join: the
+// kernels only say so (what is kept for it in their loops, or done behind them, costs them 3 to 15 %).
+constexpr float kFewLost = 16384.f;                            // 2^30 / 2^16
+// The logarithm of a denominator whose sum is relative to 2^(top - 14).
+__device__ __forceinline__ float log_of(float sum, float top) {
+  return sum == 0.f ? -INFINITY : (log2f(sum) + (top - (14.f + kLogDenominators))) * 0.69314718f;
+}
 
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -108,6 +123,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
 
+  if (blockIdx.x == 0 && tid == 0) *a.tiles_again = 0;                        // (attention_tiles comes behind this kernel)
+
   // ---- this thread block's share: all cells in one line, sequence by sequence, head by head, rows by rows
   auto scan = [&](int base, int64_t& mine) {     // this thread's sequence's cells; the sum up to and with it
     const int b = base + tid;
@@ -130,7 +147,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
   const int64_t lo = (int)blockIdx.x < blocks ? total * blockIdx.x / blocks : total;
   const int64_t hi = (int)blockIdx.x < blocks ? total * (blockIdx.x + 1) / blocks : total;
   if (lo >= hi) {
-    if (tid == 0) a.shares[blockIdx.x] = Share{total, total, total, 0, 0};
+    if (tid == 0) a.shares[blockIdx.x] = Share{total, total, total, total, 0, 0, 0, 0};
     return;
   }
   int64_t before = 0;
@@ -153,7 +170,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
     const int per = max(1, (e.reach + kCell - 1) / kCell), tiles = (int)(((int64_t)e.n * a.group + kRows - 1) / kRows);
     for (int item = (int)((pos - at) / per); pos < hi && item < c.kv_heads * tiles; ++item) {
       const int64_t start = at + (int64_t)item * per, end = start + per;
-      if (first && tid == 0) a.shares[blockIdx.x] = Share{lo, start, end, b, item};
+      if (first && tid == 0) a.shares[blockIdx.x] = Share{lo, hi, start, end, b, item, 0, 0};
       const int head = item / tiles, row0 = (item - head * tiles) * kRows;
       const int rows = min(kRows, e.n * a.group - row0);
       // keys up to the position of the row's token; a token whose position is below 0 sees none
@@ -315,13 +332,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
         if (more) load_k(cell + kWarps, next);
         // to the base 2, with the values' scales, masked
         float top[2] = {m[0], m[1]};
-        float weigh[kN], inverse[kN];
+        float weigh[kN];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          const bool tiny = cv[i] < kLeastScale;
-          weigh[i] = tiny ? -60.f : lg2(cv[i]);
-          inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
-        }
+        for (int i = 0; i < kN; ++i) weigh[i] = weigh_of(cv[i]);
 #pragma unroll
         for (int t = 0; t < kS; ++t)
 #pragma unroll
@@ -372,14 +385,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
         uint32_t p[kN][4];
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
-          const bool none = cv[n] < kLeastScale;
+          const bool none = weigh[n] < kNoValues;
+          const float inverse = ex2(kLogDenominators - weigh[n]);
           float x[2][4];                                                     // [row][key]
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
 #pragma unroll
             for (int i = 0; i < (NARROW ? 2 : 4); ++i) x[r][i] = ex2((NARROW ? s[n][2 * i + r] : s[NARROW ? 0 : 2 * n + (i >> 1)][2 * r + (i & 1)]) - from[r]);
             const float sum = NARROW ? x[r][0] + x[r][1] : (x[r][0] + x[r][1]) + (x[r][2] + x[r][3]);
-            if (sum != 0.f) l[r] = fmaf(sum, inverse[n], l[r]);               // (nothing of a block that the row does not see, whatever its scale)
+            if (sum != 0.f) l[r] = fmaf(sum, inverse, l[r]);            // (nothing of a block that the row does not see, whatever its scale)
           }
           if (NARROW) {
             p[n][0] = turned(none ? 0u : pack_half2(x[0][0], x[1][0]));
@@ -462,12 +476,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
           y.x = fmaf(x.x, by, y.x); y.y = fmaf(x.y, by, y.y); y.z = fmaf(x.z, by, y.z); y.w = fmaf(x.w, by, y.w);
         }
         if (whole) {
+          if (sum < kFewLost && top != -INFINITY) a.shares[blockIdx.x].again = 1;
           const int row = row0 + r, token = row / a.group, h = head * a.group + row - token * a.group;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          const float inv = sum == 0.f ? 0.f : kDenominators / sum;
           if (d < c.dim)
             *reinterpret_cast<uint2*>(a.out + (e.first + token) * a.ld_out + (int64_t)h * c.dim + d) =
                 make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
-          if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (top - 14.f)) * 0.69314718f;
+          if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = log_of(sum, top);
         } else {
           float* const to = a.parts + ((int64_t)slot * kMostRows + r) * (DIM + 2);
           to[d] = y.x; to[d + 1] = y.y; to[d + 2] = y.z; to[d + 3] = y.w;
@@ -481,16 +496,121 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
   }
 }
 
-// The rows whose keys several thread blocks have had, joined by the block whose share begins inside them first.  A row a thread block's quarter.
-template <int DIM>
-__global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid) {
-  pdl_prologue();
-  const int i = blockIdx.x + 1;
-  const Share s = a.shares[i];
-  if (s.lo <= s.start || s.lo >= s.end || a.shares[i - 1].lo > s.start) return;
+// One query row by a warp, in two passes over its scores: the maximum first, then every weight in fp32 from it, and the denominator's terms without
+// dv. For scales that no layer has.
+template <int FMT>
+__device__ __noinline__ void far_row(const RowsArgs& a, const Extent& e, int b, int head, int64_t row) {
   const CacheView& c = a.c;
+  const int lane = threadIdx.x & 31;
+  const int64_t token = row / a.group;
+  const __nv_bfloat16* const q = a.q + (e.first + token) * a.ld_q + ((int64_t)head * a.group + row - token * a.group) * c.dim;
+  const int end = min(e.reach, max(0, e.len - e.n + (int)token + 1));
+  float top = 0.f;
+  for (int d = lane; d < c.dim; d += 32) top = fmaxf(top, fabsf(__bfloat162float(q[d])));
+  for (int x = 16; x; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  const float scale = row_scale(top), factor = a.scale_log2 / scale;
+  auto block_of = [&](int key) {                               // -1: none
+    const int page = page_of(c, b, key >> c.shift);
+    return page < 0 ? -1ll : (long long)page * c.kv_heads + head;
+  };
+  auto at = [&](long long block, int key) { return ((block << c.shift) + (key & ((1 << c.shift) - 1))) * c.dim; };
+  // this lane's key's score to the base 2, and its values' scale
+  auto score = [&](int key, float& dv) {
+    const long long block = key < end ? block_of(key) : -1;
+    dv = 0.f;
+    if (key >= end) return -INFINITY;
+    if (block < 0) return dv = __int_as_float(0x7fffffff);
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>(c.k + at(block, key));
+    float s = 0.f;
+#pragma unroll 1
+    for (int d = 0; d < c.dim; d += 4) {
+      uint32_t h[2];
+      half4_of<FMT>(__ldg(codes + d / 4), h[0], h[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 k = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        s = fmaf(__bfloat162float(q[d + 2 * i]) * scale, k.x, s);
+        s = fmaf(__bfloat162float(q[d + 2 * i + 1]) * scale, k.y, s);
+      }
+    }
+    dv = __ldg(c.dv + block);
+    return s * (factor * __ldg(c.dk + block));
+  };
+  float most = -INFINITY, sum = 0.f;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);                  // dims 4 lane ..
+#pragma unroll 1
+  for (int k0 = 0; k0 < end; k0 += 32) {
+    float dv;
+    const float x = score(k0 + lane, dv);
+    most = fmaxf(most, x + weigh_of(dv));
+  }
+  for (int x = 16; x; x /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+  const float from = most == -INFINITY ? 0.f : most - 14.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < end; k0 += 32) {
+    float dv;
+    const float x = score(k0 + lane, dv);
+    sum += dv != dv ? dv : ex2(x - from + kLogDenominators);
+    const float p = dv < kLeastScale ? 0.f : ex2(x + weigh_of(dv) - from);
+#pragma unroll 1
+    for (int i = 0; i < 32 && k0 + i < end; ++i) {
+      const float w = __shfl_sync(0xffffffffu, p, i);
+      const long long block = block_of(k0 + i);
+      if (4 * lane >= c.dim || block < 0) continue;
+      uint32_t h[2];
+      half4_of<FMT>(__ldg(reinterpret_cast<const uint32_t*>(c.v + at(block, k0 + i)) + lane), h[0], h[1]);
+      const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&h[0])), v1 = __half22float2(*reinterpret_cast<const __half2*>(&h[1]));
+      y.x = fmaf(w, v0.x, y.x); y.y = fmaf(w, v0.y, y.y); y.z = fmaf(w, v1.x, y.z); y.w = fmaf(w, v1.y, y.w);
+    }
+  }
+  for (int x = 16; x; x /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+  const int64_t h = (int64_t)head * a.group + row - token * a.group;
+  const float inv = sum == 0.f ? 0.f : kDenominators / sum;
+  if (4 * lane < c.dim)
+    *reinterpret_cast<uint2*>(a.out + (e.first + token) * a.ld_out + h * c.dim + 4 * lane) =
+        make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+  if (lane == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = log_of(sum, most);
+}
+
+// The rows whose keys several thread blocks have had, joined by the block whose share begins inside them first; and what has to be done again.  A row
+// a thread block's quarter, or one of its warps.
+template <int FMT, int DIM>
+__global__ void __launch_bounds__(DIM) attention_join(const __grid_constant__ RowsArgs a, int grid) {
+  pdl_prologue();
+  const int i = blockIdx.x, warp = blockIdx.y * (DIM / 32) + (threadIdx.x >> 5), warps = gridDim.y * (DIM / 32);
+  const CacheView& c = a.c;
+  const Share s = a.shares[i];
+  auto tiles_of = [&](const Extent& e) { return (int)(((int64_t)e.n * a.group + a.rows - 1) / a.rows); };
+  auto item_again = [&](const Extent& e, int b, int item, int tiles) {
+    const int head = item / tiles, row0 = (item - head * tiles) * a.rows;
+    for (int r = warp; r < min(a.rows, e.n * a.group - row0); r += warps) far_row<FMT>(a, e, b, head, row0 + r);
+  };
+  if (*a.tiles_again) {                          // all rows of attention_tiles, by all warps
+    int64_t next = (int64_t)i * warps + warp;
+    for (int b = 0; b < c.batch; ++b) {
+      const Extent e = extent_of(c, b);
+      const int64_t rows = (int64_t)e.n * a.group, all = rows * c.kv_heads;
+      if (rows < a.most_rows) continue;
+      for (; next < all; next += (int64_t)gridDim.x * warps) far_row<FMT>(a, e, b, (int)(next / rows), next % rows);
+      next -= all;
+    }
+  }
+  if (s.again) {                                 // rows that it has had all of
+    int64_t at = s.start - (int64_t)s.item * (s.end - s.start);
+    int item = s.item;
+    for (int b = s.b; at < s.hi; ++b, item = 0) {
+      const Extent e = extent_of(c, b);
+      const int64_t cells = cells_of(a, e, a.rows, a.cell);
+      if (cells == 0) continue;
+      const int tiles = tiles_of(e), per = (int)(cells / ((int64_t)c.kv_heads * tiles));
+      for (; item < c.kv_heads * tiles && at + (int64_t)(item + 1) * per <= s.hi; ++item)
+        if (at + (int64_t)item * per >= s.lo) item_again(e, b, item, tiles);
+      at += cells;
+    }
+  }
+  if (i == 0 || s.lo <= s.start || s.lo >= s.end || a.shares[i - 1].lo > s.start) return;
   const Extent e = extent_of(c, s.b);
-  const int tiles = (int)(((int64_t)e.n * a.group + a.rows - 1) / a.rows), head = s.item / tiles, row0 = (s.item - head * tiles) * a.rows;
+  const int tiles = tiles_of(e), head = s.item / tiles, row0 = (s.item - head * tiles) * a.rows;
   const int rows = min(a.rows, e.n * a.group - row0), d = threadIdx.x;
   int last = i;
   while (last + 1 < grid && a.shares[last + 1].lo < s.end) ++last;
@@ -505,9 +625,13 @@ __global__ void __launch_bounds__(DIM) attention_join(const RowsArgs a, int grid
       sum = fmaf(from[DIM + 1], by, sum);
       y = fmaf(from[d], by, y);
     }
+    if (sum < kFewLost && top != -INFINITY) {    // (the same for all of the block's threads)
+      if (threadIdx.x < 32) far_row<FMT>(a, e, s.b, head, row0 + r);
+      continue;
+    }
     const int row = row0 + r, token = row / a.group, h = head * a.group + row - token * a.group;
-    if (d < c.dim) a.out[(e.first + token) * a.ld_out + (int64_t)h * c.dim + d] = __float2bfloat16_rn(sum == 0.f ? 0.f : y / sum);
-    if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (top - 14.f)) * 0.69314718f;
+    if (d < c.dim) a.out[(e.first + token) * a.ld_out + (int64_t)h * c.dim + d] = __float2bfloat16_rn(sum == 0.f ? 0.f : y * (kDenominators / sum));
+    if (d == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = log_of(sum, top);
   }
 }
 
@@ -675,14 +799,9 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
             mma16(s[u][2 * t + 1], q[u], w[t][2], w[t][3]);
           }
       }
-      float weigh[kGroups], inverse[kGroups], cv[kGroups];
+      float weigh[kGroups];
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        cv[i] = scales[buf][1][i];
-        const bool tiny = cv[i] < kLeastScale;
-        weigh[i] = tiny ? -60.f : lg2(cv[i]);
-        inverse[i] = tiny ? 1.1529215e18f : rcp(cv[i]);
-      }
+      for (int i = 0; i < kGroups; ++i) weigh[i] = weigh_of(scales[buf][1][i]);
       const bool partial = (tile + 1) * kTileKeys > least;
       uint32_t p[MT][kGroups][4];
 #pragma unroll
@@ -722,16 +841,17 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
             for (int t = 0; t < kOut; ++t) { o[u][t][2 * r] *= shrink; o[u][t][2 * r + 1] *= shrink; }
           }
         }
+        const float from[2] = {m[u][0] == -INFINITY ? 0.f : m[u][0] - 14.f, m[u][1] == -INFINITY ? 0.f : m[u][1] - 14.f};
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
-          const bool none = cv[i] < kLeastScale;
+          const bool none = weigh[i] < kNoValues;
+          const float inverse = ex2(kLogDenominators - weigh[i]);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const float base = m[u][r] == -INFINITY ? 0.f : m[u][r] - 14.f;
-            const float e0 = ex2(s[u][2 * i][2 * r] - base), e1 = ex2(s[u][2 * i][2 * r + 1] - base);
-            const float e2 = ex2(s[u][2 * i + 1][2 * r] - base), e3 = ex2(s[u][2 * i + 1][2 * r + 1] - base);
+            const float e0 = ex2(s[u][2 * i][2 * r] - from[r]), e1 = ex2(s[u][2 * i][2 * r + 1] - from[r]);
+            const float e2 = ex2(s[u][2 * i + 1][2 * r] - from[r]), e3 = ex2(s[u][2 * i + 1][2 * r + 1] - from[r]);
             const float sum = (e0 + e1) + (e2 + e3);
-            if (sum != 0.f) l[u][r] = fmaf(sum, inverse[i], l[u][r]);
+            if (sum != 0.f) l[u][r] = fmaf(sum, inverse, l[u][r]);
             p[u][i][r] = none ? 0u : pack_half2(e0, e1);
             p[u][i][2 + r] = none ? 0u : pack_half2(e2, e3);
           }
@@ -765,23 +885,25 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       const int in_warp = 16 * u + 8 * r + g;
       if (in_warp >= rows) continue;
+      if (sum < kFewLost && m[u][r] != -INFINITY) *a.tiles_again = 1;
       const int64_t row = first + in_warp, token = row / a.group, h = (int64_t)head * a.group + row - token * a.group;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const float inv = sum == 0.f ? 0.f : kDenominators / sum;
       __nv_bfloat16* const to = a.out + (e.first + token) * a.ld_out + h * c.dim;
 #pragma unroll
       for (int t = 0; t < kOut; ++t)
         if (8 * t < c.dim) *reinterpret_cast<uint32_t*>(to + 8 * t + 2 * cc) = pack_bf16x2(o[u][t][2 * r] * inv, o[u][t][2 * r + 1] * inv);
-      if (cc == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = sum == 0.f ? -INFINITY : (log2f(sum) + (m[u][r] - 14.f)) * 0.69314718f;
+      if (cc == 0 && a.lse) a.lse[(e.first + token) * a.heads + h] = log_of(sum, m[u][r]);
     }
 }
 
-constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + 255) / 256 * 256; }
+constexpr size_t share_bytes() { return (kMaxBlocks * sizeof(Share) + sizeof(int) + 255) / 256 * 256; }
 
 template <int FMT, int DIM, bool NARROW>
-qm_status launch_rows(RowsArgs a, cudaStream_t s) {
+qm_status launch_rows(RowsArgs& a, int* grid, cudaStream_t s) {
   constexpr auto kern = attention_rows<FMT, DIM, NARROW>;
   constexpr size_t smem = (size_t)kWarps * (NARROW ? 8 : 16) * (DIM + 4) * 4;
   a.rows = NARROW ? 8 : 16;
+  a.cell = cell_of(DIM, NARROW);
   static std::atomic<int> resident[kMaxDevices];
   const int dev = current_device();
   if (dev < 0) return QM_ERR_UNSUPPORTED;
@@ -794,10 +916,7 @@ qm_status launch_rows(RowsArgs a, cudaStream_t s) {
   }
   QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)most), dim3(kWarps * 32), smem, s, a));
   count_launch();
-  if (most > 1) {
-    QM_CUDA_OK(launch_pdl(attention_join<DIM>, dim3((unsigned)most - 1, 4), dim3(DIM), 0, s, a, most));
-    count_launch();
-  }
+  *grid = most;
   return QM_OK;
 }
 template <int FMT, int DIM, int MT>
@@ -823,12 +942,14 @@ qm_status launch_both(RowsArgs a, cudaStream_t s) {
   const int64_t blocks = a.c.tokens * a.group / 128 * a.c.kv_heads;
   const bool tiles = (a.c.tokens - a.c.batch + 1) * a.group >= 64 && blocks >= sm_count() / 3 && a.c.kv_heads < 65536;
   a.most_rows = tiles ? 64 : 0x7fffffff;
-  if (tiles) {
-    const qm_status st = blocks >= 2 * sm_count() ? launch_tiles<FMT, DIM, 2>(a, s) : launch_tiles<FMT, DIM, 1>(a, s);
-    if (st != QM_OK) return st;
-  }
   // eight rows to a cell where a sequence has no more on the average
-  return a.c.tokens * a.group <= 8ll * a.c.batch ? launch_rows<FMT, DIM, true>(a, s) : launch_rows<FMT, DIM, false>(a, s);
+  int grid = 0;
+  qm_status st = a.c.tokens * a.group <= 8ll * a.c.batch ? launch_rows<FMT, DIM, true>(a, &grid, s) : launch_rows<FMT, DIM, false>(a, &grid, s);
+  if (st == QM_OK && tiles) st = blocks >= 2 * sm_count() ? launch_tiles<FMT, DIM, 2>(a, s) : launch_tiles<FMT, DIM, 1>(a, s);
+  if (st != QM_OK) return st;
+  QM_CUDA_OK(launch_pdl(attention_join<FMT, DIM>, dim3((unsigned)grid, 4), dim3(DIM), 0, s, a, grid));
+  count_launch();
+  return QM_OK;
 }
 template <int FMT>
 qm_status launch_dim(const RowsArgs& a, cudaStream_t s) { return a.c.dim <= 64 ? launch_both<FMT, 64>(a, s) : launch_both<FMT, 128>(a, s); }
@@ -845,6 +966,7 @@ qm_status launch_cache_attention(const CacheArgs& c, const AttentionArgs& l, cud
   a.scale_log2 = l.scale * 1.44269504f;
   a.out = static_cast<__nv_bfloat16*>(l.out); a.ld_out = l.ld_out; a.lse = l.lse;
   a.shares = static_cast<Share*>(l.ws);
+  a.tiles_again = reinterpret_cast<int*>(a.shares + kMaxBlocks);
   a.parts = reinterpret_cast<float*>(static_cast<char*>(l.ws) + share_bytes());
   return c.fmt == QM_FMT_INT8 ? launch_dim<QM_FMT_INT8>(a, s) : c.fmt == QM_FMT_E4M3 ? launch_dim<QM_FMT_E4M3>(a, s) : launch_dim<QM_FMT_E5M2>(a, s);
 }
