@@ -49,6 +49,7 @@ struct Share { int64_t lo, hi, start, end; int b, item, again, pad; };
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+__device__ __forceinline__ float key_scale(float dk) { return dk < kLeastScale ? 0.f : dk; }
 // Blocks' scales may lie far apart, and both sums are relative to one maximum that has dv in it, which a denominator's terms may be far above or
 // below. 2^16 / dv is what they are multiplied with: for dv from 2^-61 to 2^128 that, and the sums from a weight of 1 to 2^31 of them, are normal numbers
 // (2^-112 .. 2^77, 2^-98 .. 2^122). weigh_of: log2 dv, of what counts as 0 less than any other's.
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
           }
         float ck[kN], cv[kN];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) { ck[i] = dk[i]; cv[i] = dv[i]; }
+        for (int i = 0; i < kN; ++i) { ck[i] = key_scale(dk[i]); cv[i] = dv[i]; }
         const bool more = cell + kWarps < cell1;
         if (more) load_k(cell + kWarps, next);
         // to the base 2, with the values' scales, masked
@@ -534,7 +535,7 @@ __device__ __noinline__ void far_row(const RowsArgs& a, const Extent& e, int b, 
       }
     }
     dv = __ldg(c.dv + block);
-    return s * (factor * __ldg(c.dk + block));
+    return s * (factor * key_scale(__ldg(c.dk + block)));
   };
   float most = -INFINITY, sum = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);                  // dims 4 lane ..
@@ -761,7 +762,7 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + x * kTileKeys * kPitch + 16 * j), "r"(h[4 * j]), "r"(h[4 * j + 1]),
                        "r"(h[4 * j + 2]), "r"(h[4 * j + 3]) : "memory");
       }
-    if (tid < 2 * kGroups) scales[buf][tid / kGroups][tid % kGroups] = scale;
+    if (tid < 2 * kGroups) scales[buf][tid / kGroups][tid % kGroups] = tid < kGroups ? key_scale(scale) : scale;
   };
   pages(0);
   load(0);

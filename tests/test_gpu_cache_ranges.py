@@ -62,3 +62,21 @@ def test_scores_far_apart_where_scales_are(kv, group, dim, block, new, lens):
     held = np.isfinite(case.dv)
     case.dv[held] = np.exp2(case.rng.choice([-59.0, -20.0, 60.0, 110.0], case.dv.shape))[held].astype(np.float32)
     check(case, kv * group)
+
+
+@pytest.mark.parametrize("kv,group,dim,block,new,lens", SHAPES)
+@pytest.mark.parametrize("fmt", ["int8", "e5m2"])
+def test_scales_of_keys_below_the_least_count_as_zero(kv, group, dim, block, new, lens, fmt):
+    """Queries so large that keys of 2^-60 give scores of a few units: those below that are keys of zeros, others are not."""
+    case = Case(fmt, kv, dim, block, new, lens, seed=7).fill(lens)
+    held = np.isfinite(case.dk)
+    top = {"int8": 127.0, "e5m2": 57344.0}[fmt]
+    case.dk[held] = np.exp2(case.rng.choice([-62.0, -60.5, -60.0, -59.5], case.dk.shape))[held].astype(np.float32)
+    check(case, kv * group, q_scale=2.0 ** 61 / top, scale=2 * dim ** -0.5)
+
+
+def test_oracle_counts_least_scales_as_zero():
+    codes = np.arange(1, 17, dtype=np.uint8).reshape(1, 1, 16, 1).repeat(16, 3)
+    one, low, q = np.ones((1, 1), np.float32), np.full((1, 1), 2.0 ** -61, np.float32), np.full((1, 1, 16), 2.0 ** 60, np.float32)
+    out, lse, _ = blocks.cache_attention(q, codes, low, codes, one, np.array([[0]]), [16], [0, 1], "int8", 1.0)
+    assert np.allclose(out, 8.5) and np.allclose(lse, np.log(16))
