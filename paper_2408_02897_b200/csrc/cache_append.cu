@@ -3,7 +3,7 @@
 // A block of tokens and a head have one scale, delta = max|x| / qmax over what the block has held; where new tokens raise it, the
 // codes that are there already are rounded again under the new one.  One unit of work is a touched block, a head, and keys or values: it
 // finds the new tokens' maximum, then writes codes.  Bound by HBM for prompts (the new tokens are read once from there and once
-// from L1 or L2; 8 prompts of up to 1000 tokens, 16 heads of 64, 14.7 us), by latency for a token at a time (64 tokens, 8 heads of 128, 3.1 us).
+// from L1 or L2; 8 prompts of up to 1000 tokens, 16 heads of 64, 15.6 us), by latency for a token at a time (64 tokens, 8 heads of 128, 2.9 us).
 #include "cache_device.cuh"
 
 namespace qm {
@@ -13,8 +13,15 @@ struct AppendArgs {
   CacheView c;
   const void *k, *v;
   int64_t ld_k, ld_v;              // elements between tokens
-  int64_t units;                   // (block, head)
 };
+
+// The blocks that a sequence's new tokens touch, from `first` on; none if it has no tokens or they have no positions.
+struct Touched { int first, n; };
+__device__ __forceinline__ Touched touched_by(const CacheView& c, const Extent& e) {
+  if (e.n == 0 || e.len == 0) return {0, 0};
+  const int first = max(e.len - e.n, 0) >> c.shift;
+  return {first, ((e.len - 1) >> c.shift) - first + 1};
+}
 
 template <int FMT>
 __device__ __noinline__ uint32_t append_far(float x0, float x1, float delta) {
@@ -52,25 +59,25 @@ template <typename T, int FMT, int THREADS>
 __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
   pdl_prologue();
   const CacheView& c = a.c;
-  const int64_t unit = (int64_t)blockIdx.x * (128 / THREADS) + threadIdx.x / THREADS;
-  if (unit >= a.units) return;
-  const int tid = threadIdx.x % THREADS, head = (int)(unit % c.kv_heads);
-  const int64_t cand = unit / c.kv_heads;
-  // Sequence b has the candidates from starts[b] / block_tokens + 2 b on, at least as many as the blocks that it touches.
-  int lo = 0, hi = c.batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    const int64_t from = ((c.starts ? c.starts[mid] : mid) >> c.shift) + 2ll * mid;
-    if (from <= cand) lo = mid; else hi = mid - 1;
+  const int tid = threadIdx.x % THREADS;
+  auto units_of = [&](int b) { return touched_by(c, extent_of(c, b)).n * c.kv_heads; };
+  // all sequences' units in one line; without `starts` a sequence has one block, or no position
+  const int first = blockIdx.x * (128 / THREADS), unit = first + threadIdx.x / THREADS;
+  Place at{unit / c.kv_heads, unit - unit % c.kv_heads, c.kv_heads};
+  if (c.starts) {
+    at = place_of<128>(c.batch, first, units_of);
+    if (at.b < 0) return;
+    while (unit >= at.begin + at.n && ++at.b < c.batch) { at.begin += at.n; at.n = units_of(at.b); }
   }
-  const int b = lo;
-  const int64_t j = cand - ((c.starts ? c.starts[b] : b) >> c.shift) - 2ll * b;
+  if (at.b >= c.batch) return;
+  const int head = (unit - at.begin) % c.kv_heads, b = at.b;
   const Extent e = extent_of(c, b);
+  const Touched touched = touched_by(c, e);
+  if (touched.n == 0) return;
+  const int block = touched.first + (unit - at.begin) / c.kv_heads;
   const int64_t p0 = max((int64_t)e.len - e.n, (int64_t)0);                  // position of the first new token (those before 0 have none)
-  const int64_t block = (p0 >> c.shift) + j;
-  if (e.n == 0 || j < 0 || block > ((int64_t)e.len - 1) >> c.shift || e.len == 0) return;
-  const int64_t from = max(p0, block << c.shift), to = min((int64_t)e.len, (block + 1) << c.shift);
-  const int page = page_of(c, b, (int)block);
+  const int64_t from = max(p0, (int64_t)block << c.shift), to = min((int64_t)e.len, ((int64_t)block + 1) << c.shift);
+  const int page = page_of(c, b, block);
   if (page < 0) return;
   const int slot = (int)(from & ((1 << c.shift) - 1)), n = (int)(to - from);
   const int64_t token = e.first + (from - ((int64_t)e.len - e.n));
@@ -78,9 +85,9 @@ __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
   const bool values = blockIdx.y;
   const T* const x = static_cast<const T*>(values ? a.v : a.k) + token * (values ? a.ld_v : a.ld_k) + (int64_t)head * c.dim;
   const int64_t ld = values ? a.ld_v : a.ld_k;
-  const int64_t at = (int64_t)page * c.kv_heads + head;
-  uint8_t* const codes = (values ? c.v : c.k) + (at << c.shift) * c.dim;
-  float* const delta = (values ? c.dv : c.dk) + at;
+  const int64_t place = (int64_t)page * c.kv_heads + head;
+  uint8_t* const codes = (values ? c.v : c.k) + (place << c.shift) * c.dim;
+  float* const delta = (values ? c.dv : c.dk) + place;
   const int per = c.dim / 8, work = n * per;                                 // eight elements at a time
 
   uint32_t top = 0;
@@ -115,19 +122,19 @@ __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
 }
 
 template <typename T, int FMT>
-qm_status launch_typed(const AppendArgs& a, cudaStream_t s) {
+qm_status launch_typed(const AppendArgs& a, int64_t units, cudaStream_t s) {
   // a warp where a unit has a token or two, as when one is generated at a time
   if (a.c.tokens <= 2ll * a.c.batch) {
-    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 32>, dim3((unsigned)((a.units + 3) / 4), 2), dim3(128), 0, s, a));
+    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 32>, dim3((unsigned)((units + 3) / 4), 2), dim3(128), 0, s, a));
   } else {
-    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 128>, dim3((unsigned)a.units, 2), dim3(128), 0, s, a));
+    QM_CUDA_OK(launch_pdl(cache_append_kernel<T, FMT, 128>, dim3((unsigned)units, 2), dim3(128), 0, s, a));
   }
   count_launch();
   return QM_OK;
 }
 template <typename T>
-qm_status launch_format(const AppendArgs& a, int fmt, cudaStream_t s) {
-  return fmt == QM_FMT_INT8 ? launch_typed<T, QM_FMT_INT8>(a, s) : fmt == QM_FMT_E4M3 ? launch_typed<T, QM_FMT_E4M3>(a, s) : launch_typed<T, QM_FMT_E5M2>(a, s);
+qm_status launch_format(const AppendArgs& a, int64_t units, int fmt, cudaStream_t s) {
+  return fmt == QM_FMT_INT8 ? launch_typed<T, QM_FMT_INT8>(a, units, s) : fmt == QM_FMT_E4M3 ? launch_typed<T, QM_FMT_E4M3>(a, units, s) : launch_typed<T, QM_FMT_E5M2>(a, units, s);
 }
 
 }  // namespace
@@ -136,9 +143,10 @@ qm_status launch_cache_append(const CacheArgs& c, const void* k, int64_t ld_k, c
   AppendArgs a{};
   a.c = view_of(c);
   a.k = k; a.v = v; a.ld_k = ld_k; a.ld_v = ld_v;
-  a.units = ((c.tokens >> a.c.shift) + 2 * c.batch) * c.kv_heads;
-  if (a.units >= (1ll << 31)) return QM_ERR_UNSUPPORTED;
-  return dtype == QM_DT_BF16 ? launch_format<__nv_bfloat16>(a, c.fmt, s) : launch_format<float>(a, c.fmt, s);
+  // at most (sequences' rows of the tokens do not overlap): a sequence's tokens touch a block for each block_tokens of them and two more
+  const int64_t units = (c.starts ? (c.tokens >> a.c.shift) + 2 * c.batch : c.batch) * c.kv_heads;
+  if (units >= (1ll << 31) - 4) return QM_ERR_UNSUPPORTED;
+  return dtype == QM_DT_BF16 ? launch_format<__nv_bfloat16>(a, units, c.fmt, s) : launch_format<float>(a, units, c.fmt, s);
 }
 
 }  // namespace qm

@@ -40,6 +40,47 @@ __device__ __forceinline__ int page_of(const CacheView& c, int b, int i) {
   return p >= 0 && p < c.blocks ? p : -1;
 }
 
+// Items of all sequences in one line, sequence b's count(b) of them behind those before it, less than 2^31 in all: the sequence b that has item `want`
+// (-1: none), where its items begin and how many they are. Goes by each sequence's checked extent, so that what one sequence's entries say moves no
+// other's items. For all threads of a block.
+struct Place { int b, begin, n; };
+template <int THREADS, typename Count>
+__device__ __forceinline__ Place place_of(int batch, int want, Count count) {
+  __shared__ int sums[THREADS / 32];
+  __shared__ Place place;
+  constexpr int kEach = 4;                                     // neighbouring sequences to a thread, where there are many
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = batch <= THREADS ? 1 : kEach;
+  if (tid == 0) place = Place{-1, 0, 0};
+  int before = 0;
+  for (int base = 0; base < batch && before <= want; base += THREADS * each) {
+    const int b0 = base + tid * each;
+    int mine[kEach], up = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      mine[i] = i < each && b0 + i < batch ? count(b0 + i) : 0;
+      up += mine[i];
+    }
+    const int all = up;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += t; }
+    if (lane == 31) sums[warp] = up;
+    __syncthreads();
+    int begin = before + up - all;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) begin += sums[w];
+      before += sums[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (begin <= want && want < begin + mine[i]) place = Place{b0 + i, begin, mine[i]};
+      begin += mine[i];
+    }
+    __syncthreads();
+  }
+  return place;
+}
+
 // Two codes (the low 16 bits) as two fp16; all of them are on fp16's grid.
 template <int FMT>
 __device__ __forceinline__ uint32_t half2_of(uint32_t two) {
