@@ -652,7 +652,7 @@ __device__ __forceinline__ void ldmatrix4_turned(uint32_t (&r)[4], uint32_t addr
 // MT: times 16 rows a warp.  An operand of keys or values is 256 bytes of shared memory for a product of eight cycles a scheduler, which with 16 rows
 // is all that shared memory gives; 32 rows use it twice.
 template <int FMT, int DIM, int MT>
-__global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const RowsArgs a, int64_t candidates) {
+__global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const RowsArgs a) {
   constexpr int kTileRows = 128 * MT, kPitch = DIM * 2 + 16, kSteps = DIM / 16, kOut = DIM / 8;
   static_assert(kTileKeys * DIM / 16 <= 256, "a 16-byte piece of the keys to a thread");
   extern __shared__ __align__(16) uint8_t tile_raw[];                          // [2 buffers][keys, values][kTileKeys][kPitch], queries [kTileRows][kPitch]
@@ -660,19 +660,16 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) attention_tiles(const Ro
   pdl_prologue();
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, cc = lane & 3;
-  // Sequence b has the candidates from starts[b] group / kTileRows + b on, at least as many as its tiles.  The last ones, which see most, come first.
+  // All sequences' tiles in one line from its end: the last ones, which see most, come first.
   const int head = blockIdx.y;
-  const int64_t cand = candidates - 1 - blockIdx.x;
-  auto from_of = [&](int i) { return (int64_t)(c.starts ? c.starts[i] : i) * a.group / kTileRows + i; };
-  int lo = 0, hi = c.batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (from_of(mid) <= cand) lo = mid; else hi = mid - 1;
-  }
-  const int b = lo;
+  const Place at = place_of<256>(c.batch, blockIdx.x, [&](int i) {
+    const int64_t rows = (int64_t)extent_of(c, c.batch - 1 - i).n * a.group;
+    return rows < a.most_rows ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
+  });
+  if (at.b < 0) return;
+  const int b = c.batch - 1 - at.b;
   const Extent e = extent_of(c, b);
-  const int64_t row0 = (cand - from_of(b)) * kTileRows, all = (int64_t)e.n * a.group;
-  if (all < a.most_rows || row0 < 0 || row0 >= all) return;
+  const int64_t row0 = (int64_t)(at.n - 1 - ((int)blockIdx.x - at.begin)) * kTileRows, all = (int64_t)e.n * a.group;
 
   auto limit_of = [&](int64_t r) { return r < all ? min(e.reach, max(0, e.len - e.n + (int)(r / a.group) + 1)) : 0; };
   const int64_t first = row0 + 16 * MT * warp;                                 // of this warp; may be beyond the last
@@ -930,8 +927,9 @@ qm_status launch_tiles(const RowsArgs& a, cudaStream_t s) {
     QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tiles_smem<DIM>(MT)));
     ready[dev].store(true, std::memory_order_relaxed);
   }
-  const int64_t candidates = a.c.tokens * a.group / (128 * MT) + a.c.batch;
-  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)candidates, (unsigned)a.c.kv_heads), dim3(256), tiles_smem<DIM>(MT), s, a, candidates));
+  // at most (sequences' rows of the tokens do not overlap): every 128 MT rows, and one more for each sequence
+  const int64_t most = a.c.tokens * a.group / (128 * MT) + a.c.batch;
+  QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)most, (unsigned)a.c.kv_heads), dim3(256), tiles_smem<DIM>(MT), s, a));
   count_launch();
   return QM_OK;
 }

@@ -47,6 +47,26 @@ def test_append(starts, tokens, lens, kv, dim, block):
         assert np.array_equal(d[name].cpu().numpy(), want, equal_nan=name.endswith("delta")), name
 
 
+@pytest.mark.parametrize("starts,tokens,lens", STARTS)
+@pytest.mark.parametrize("kv,group,dim,block", [(1, 2, 64, 16), (16, 2, 64, 32), (32, 4, 128, 16)])      # the last two: tiles, if there are tokens enough
+def test_attention(starts, tokens, lens, kv, group, dim, block):
+    case, valid = case_of(starts, tokens, lens, kv, dim, block, "int8")
+    case.fill(lens)
+    q, qd = case.queries(kv * group)
+    out = torch.full((tokens, kv * group, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    before = qm.kernel_launches()
+    qm.qm_cache_attention(qd, **case.device(), out=out)
+    assert qm.kernel_launches() - before == (3 if kv > 1 and tokens >= 130 else 2)      # tiles, rows, join
+    q, out, rest = q.float().numpy(), out.double().cpu().numpy(), np.ones(tokens, bool)
+    for b, first, end in valid:
+        want, _, top = blocks.cache_attention(q, case.k, case.dk, case.v, case.dv, case.tables[b:b + 1], case.lens[b:b + 1], [first, end], "int8", dim ** -0.5)
+        tol, _ = attention_tolerance(case, q, want, top, dim ** -0.5)
+        rows = slice(first, end)
+        assert (np.abs(out - want) <= tol)[rows].all(), b
+        rest[rows] = False
+    assert (out[rest] == 7.0).all()
+
+
 def test_append_to_very_many_sequences():
     """More units of work than thread blocks: several to each, of sequences with nothing, one or several tokens and entries that name no rows."""
     rng = np.random.default_rng(4)
