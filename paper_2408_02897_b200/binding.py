@@ -423,6 +423,14 @@ def _blocks(n, side=SCALE_BLOCK):
     return (n + side - 1) // side
 
 
+def _scales(t, what, rows, cols, device):
+    """Address of contiguous scales [rows, cols], or of as many in one dimension. The other order, [cols, rows], is refused where it is another one."""
+    shape = t.shape
+    if shape != (rows, cols) and len(shape) > 1 and [n for n in shape if n != 1] != [n for n in (rows, cols) if n != 1]:
+        _refuse(f"{what}: wants [{rows}, {cols}], not {list(shape)}")
+    return _vector(t, what, rows * cols, _FP32, device)
+
+
 def qm_quantize_blocks(op, fmt, side=1, stream=None):
     """FP8 codes of a 2-D operand with a scale for each 128 contraction entries of `side` rows (1 or 128):
     (codes [rows, qm_code_ld(K)], delta [ceil(K / 128), ceil(rows / side)]), as qm_linear_fp8 takes them."""
@@ -450,8 +458,7 @@ def qm_linear_fp8(codes_x, delta_x, codes_w, delta_w, K, fmt_x="e4m3", fmt_w="e4
         _refuse(f"side_w: 1 or {SCALE_BLOCK}")
     M, ld_x = _codes(codes_x, "codes_x", K, device)
     N, ld_w = _codes(codes_w, "codes_w", K, device)
-    dx = _vector(delta_x, "delta_x", _blocks(K) * M, _FP32, device)
-    dw = _vector(delta_w, "delta_w", _blocks(K) * _blocks(N, side_w), _FP32, device)
+    dx, dw = _scales(delta_x, "delta_x", _blocks(K), M, device), _scales(delta_w, "delta_w", _blocks(K), _blocks(N, side_w), device)
     b = _vector(bias, "bias", N, _FLOATS, device) if bias is not None else None
     out, ld = _linear_out(out, out_dtype, M, N, codes_x, stream, device)
     st = lib().qm_linear_fp8(codes_x.data_ptr(), ld_x, FMT[fmt_x], dx, codes_w.data_ptr(), ld_w, FMT[fmt_w], dw, side_w, b,
@@ -473,7 +480,7 @@ def _cache(k_codes, k_delta, v_codes, v_delta, tables, lens, starts, fmt, device
     n = blocks * kv_heads * block_tokens * dim
     batch, width, ld = _matrix(tables, "tables", _INTS, device)
     return Cache(_vector(k_codes, "k_codes", n, _BYTES, device), _vector(v_codes, "v_codes", n, _BYTES, device),
-                 _vector(k_delta, "k_delta", blocks * kv_heads, _FP32, device), _vector(v_delta, "v_delta", blocks * kv_heads, _FP32, device),
+                 _scales(k_delta, "k_delta", blocks, kv_heads, device), _scales(v_delta, "v_delta", blocks, kv_heads, device),
                  blocks, kv_heads, block_tokens, dim, FMT[fmt], tables.data_ptr(), ld, width, batch,
                  _vector(lens, "lens", batch, _INTS, device),
                  _vector(starts, "starts", batch + 1, _INTS, device) if starts is not None else None)
