@@ -512,7 +512,7 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       uint64_t acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0;
-      for (int kb = 0; kb < a.num_kb; ++kb, ++it) {
+      for (int kb = 0; kb < a.num_kb && ok; ++kb, ++it) {
         const uint32_t buf = it & 1, from = tmem_base + ((uint32_t)(q * 32) << 16) + buf * 256 + h * 128;
         copies_wait<kAhead - 2>();
         __syncwarp();                                                         // (and the slot that is filled next has been read by all lanes)
@@ -526,7 +526,9 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           for (int i = 0; i < 4; ++i) d[c & 1][SIDE1 ? i : 0] = *reinterpret_cast<const float4*>(sc + 32 + 16 * c + 4 * i);
         };
         if (SIDE1) columns(0);
-        ok = ok && w.wait_warp(smem_u32(&sh->sum_full[buf]), (it >> 1) & 1);
+        // (a warp that gives up arrives no more: an arrival for sums that it has not read would let others be overwritten that a peer yet reads)
+        ok = w.wait_warp(smem_u32(&sh->sum_full[buf]), (it >> 1) & 1);
+        if (!ok) break;
         tc_fence_after();
         uint32_t r[2][16];
         tmem_ld16(from, r[0]);
@@ -590,6 +592,7 @@ linear_fp8_many(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
       }
     }
+    copies_wait<0>();                                                         // (of scales that a kernel which gives up has not used)
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
 
