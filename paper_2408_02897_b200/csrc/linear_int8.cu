@@ -634,7 +634,7 @@ linear_many_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->tmem_empty[buf]), 0));
+      if (lane == 0 && ok) mbar_arrive_cluster(map_to_cta(smem_u32(&sh->tmem_empty[buf]), 0));      // (as in linear_fp8_many: no arrival for what was not read)
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
