@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
       auto limit_of = [&](int r) { return r < rows ? min(e.reach, max(0, e.len - e.n + (row0 + r) / a.group + 1)) : 0; };
       const int limit[2] = {limit_of(NARROW ? 2 * cc : g), limit_of(NARROW ? 2 * cc + 1 : g + 8)};      // of the rows whose statistics this thread has
       const int least = limit_of(0), most = limit_of(rows - 1);
-      // (a 64-bit min(end, hi) in place of the choice was compiled to per in all but a share's first rows: nvcc 12.9)
+      // (written as min(end, hi) - start this is compiled to per in all but a share's first rows, as recorded in the kernel: nvcc 12.9.86, at ptxas' -O1
+      // too. The tests of single tokens show it; the same walk by itself, without the products, does not.)
       const int cell0 = (int)(pos - start), quota = hi < end ? (int)(hi - start) : per, cell1 = min(quota, (most + kCell - 1) / kCell);
 
       // ---- queries: row g, or rows g and g + 8, in the order of dims in which a thread has its part of a key
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attention_rows(const RowsArgs 
         }
       }
       first = false;
-      pos = min(end, hi);
+      pos = end;                                                         // (at or beyond hi: the loops end)
     }
     at += mine_all;
   }
