@@ -928,8 +928,8 @@ qm_status launch_tiles(const RowsArgs& a, cudaStream_t s) {
     QM_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tiles_smem<DIM>(MT)));
     ready[dev].store(true, std::memory_order_relaxed);
   }
-  // at most (sequences' rows of the tokens do not overlap): every 128 MT rows, and one more for each sequence
-  const int64_t most = a.c.tokens * a.group / (128 * MT) + a.c.batch;
+  // at most (sequences' rows of the tokens do not overlap): every 128 MT rows, and one more for each sequence that has most_rows or more
+  const int64_t rows = a.c.tokens * a.group, most = rows / (128 * MT) + std::min<int64_t>(a.c.batch, rows / a.most_rows);
   QM_CUDA_OK(launch_pdl(kern, dim3((unsigned)most, (unsigned)a.c.kv_heads), dim3(256), tiles_smem<DIM>(MT), s, a));
   count_launch();
   return QM_OK;
@@ -937,10 +937,14 @@ qm_status launch_tiles(const RowsArgs& a, cudaStream_t s) {
 
 // Which sequences are whose: attention_tiles takes those with 64 query rows of a cached head or more, if the call has enough of them to give a third
 // of the SMs 128 rows; its thread blocks do not share keys, attention_rows does, whatever the rows.  256 rows to a thread block where there are enough for all SMs.
+// How many rows one sequence has only the device knows: all of the call's, at most, but where there are as many tokens as sequences a token of each is
+// taken for granted. (Beside sequences without new tokens, us without attention_tiles / with it: 1000 tokens on 2000 among 1023, 32 heads on 8 of 128, 386 / 162;
+// 300 on 2000 among 400, 64 heads of 64, 147 / 97; in vain: 512 single tokens on 500, 32 heads on 8 of 128, 162 / 169.)
 template <int FMT, int DIM>
 qm_status launch_both(RowsArgs a, cudaStream_t s) {
   const int64_t blocks = a.c.tokens * a.group / 128 * a.c.kv_heads;
-  const bool tiles = (a.c.tokens - a.c.batch + 1) * a.group >= 64 && blocks >= sm_count() / 3 && a.c.kv_heads < 65536;
+  const int64_t most_tokens = a.c.tokens == a.c.batch ? 1 : a.c.tokens;
+  const bool tiles = most_tokens * a.group >= 64 && blocks >= sm_count() / 3 && a.c.kv_heads < 65536;
   a.most_rows = tiles ? 64 : 0x7fffffff;
   // eight rows to a cell where a sequence has no more on the average
   int grid = 0;

@@ -48,3 +48,14 @@ def test_lengths_beyond_the_table_in_tiles(dim, kv, group, tokens):
 def test_shares_that_begin_and_end_inside_rows(kv, group, dim, block, new, lens, fmt):
     """Thread blocks' equal shares of keys cross heads and sequences: none is skipped or taken twice (a log-sum-exp would be off by its logarithm)."""
     check_attention(Case(fmt, kv, dim, block, new, lens, seed=kv + dim).fill(lens), kv * group)
+
+
+def test_a_prompt_among_sequences_without_new_tokens():
+    """The rows of a call are one sequence's, however many others there are without any."""
+    new, lens = [0] * 150 + [200] + [0] * 149, [5] * 150 + [300] + [33] * 149
+    case = Case("int8", 64, 64, 32, new, lens, seed=3).fill(lens)
+    q, qd = case.queries(64)
+    _, n = launches(lambda: qm.qm_cache_attention(qd, **case.device()))
+    assert n == 3
+    small = Case("int8", 16, 64, 32, new, lens, seed=3).fill(lens)
+    check_attention(small, 64)
