@@ -81,20 +81,7 @@ __device__ __forceinline__ Place place_of(int batch, int want, Count count) {
   return place;
 }
 
-// Two codes (the low 16 bits) as two fp16; all of them are on fp16's grid.
-template <int FMT>
-__device__ __forceinline__ uint32_t half2_of(uint32_t two) {
-  uint32_t h;
-  if (FMT == QM_FMT_E4M3) asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(h) : "r"(two));
-  else if (FMT == QM_FMT_E5M2) h = __byte_perm(two, 0u, 0x1404);                 // the upper half of an fp16
-  else {
-    // 1024 + (code + 128) is 0x6400 | (code ^ 0x80)
-    const uint32_t u = __byte_perm(two ^ 0x8080u, 0x64646464u, 0x4140);
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(u), "r"(0x64806480u));
-  }
-  return h;
-}
-// Four codes as two pairs.
+// Four codes as two pairs of fp16; all of them are on fp16's grid.
 template <int FMT>
 __device__ __forceinline__ void half4_of(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if (FMT == QM_FMT_E4M3) {
