@@ -349,7 +349,8 @@ qm_status qm_gated_linear_int8(const uint8_t* codes_x, int64_t ld_x, const float
  *
  * qm_quantize_blocks: Eq. 1 over each block of `side` rows (non-contracting indices; 1 or 128, the last block may be smaller) and 128 contraction
  * entries: delta = max|x| / qmax, codes = sat(RTNE(x / delta)) as qm_quantize gives them under that scale.
- *  x          a 2-D operand (batch 1), either dimension contiguous, bf16 or fp32
+ *  x          a 2-D operand (batch 1), either dimension contiguous, bf16 or fp32; up to 65535 blocks of the contraction, and of rows where
+ *             side is 128 and the contraction contiguous (65535 * 128 entries; QM_ERR_UNSUPPORTED beyond)
  *  fmt        QM_FMT_E4M3 or QM_FMT_E5M2
  *  delta      device fp32 [ceil(contract / 128)][ceil(noncontract / side)]
  *  codes      device bytes [noncontract][qm_code_ld(contract)], the contracting index contiguous, padding zero, 16-byte aligned
@@ -385,10 +386,12 @@ qm_status qm_linear_fp8(const uint8_t* codes_x, int64_t ld_x, int32_t fmt_x, con
  *  starts             device int32 [batch + 1]: sequence b's new tokens are rows starts[b] .. starts[b + 1] - 1 of k, v and q, its last tokens in
  *                     that order; a sequence may have none.  NULL: one for each sequence (tokens = batch).
  *  fmt                qm_format, of keys and values alike
- * block_tokens is a power of two from 16 to 256, head_dim a multiple of 16 up to 128.  A block must not be in two places of the tables if one of
- * them is written.  Scales are at least 0; one below 2^-60 counts as 0.  What tables, lens and starts say is checked on the device: a
- * sequence whose rows of `starts` are not inside 0 .. tokens has no new tokens, a position below 0 does not exist, and no block
- * outside 0 .. blocks - 1 or beyond the table is touched.
+ * block_tokens is a power of two from 16 to 256, head_dim a multiple of 16 up to 128, kv_heads at most 65536, table_width * block_tokens at
+ * most 2^31 - 65536.  A block must not be in two places of the tables if one of them is written.  Scales are finite and at least 0; one below
+ * 2^-60 counts as 0.  What tables, lens and starts say is checked on the device: a sequence whose rows of `starts` are not inside
+ * 0 .. tokens, in that order, has no new tokens, whatever the sequences beside it have (entries need not rise: what is behind the last sequence may be
+ * zeros); a position below 0 does not exist, and no block outside 0 .. blocks - 1 or beyond the table is touched.  No row belongs to two
+ * sequences: of ones that overlap, some may be left out.
  */
 typedef struct {
   uint8_t* k_codes;
@@ -424,8 +427,10 @@ qm_status qm_cache_append(const qm_cache* cache, const void* k, int64_t ld_k, co
  *  ws       device scratch of at least qm_cache_attention_workspace_bytes(head_dim) bytes, 256-byte aligned; its contents do not matter and
  *           concurrent calls must not share it (nor two captured graphs that may run at the same time)
  * A token whose position is below 0 sees nothing: out 0, lse -inf.  One that sees a token of a block with a NaN scale, or of a
- * position that has no block, gets NaN.  Codes of tokens that nothing new sees, and their scales, may be anything.  The weights are rounded to fp16's 11 bits ahead of their
- * product with the values; scores, statistics and sums are fp32.  The same call gives the same bits each time.
+ * position that has no block, gets NaN.  Codes of tokens that nothing new sees, and their scales, may be anything.  The same call gives the same bits each time.
+ * Scores, statistics and sums are fp32; a score beyond fp32 gives NaN.  A weight times its values' scale is rounded to fp16's 11 bits ahead of its product with the
+ * codes, 2^-11 of it, or 2^-39 of the row's largest where it is small.  Exponentials, and the logarithm of a value scale, are the hardware's approximate
+ * ones: relative errors of a few 2^-22, and of 2^-24 for each power of two that a scale lies from 1.
  */
 size_t qm_cache_attention_workspace_bytes(int32_t head_dim);
 qm_status qm_cache_attention(const qm_cache* cache, const void* q, int64_t ld_q, int32_t heads, float scale, int64_t tokens, void* out,
@@ -640,7 +645,7 @@ qm_status qm_debug_read_pass(const void* data, size_t bytes, int32_t variant, in
  * of the contraction; where probes share their products, a tile's slices of the
  * operands, then 128-deep ones of each probe's codes), so that the warps waiting
  * for the next slice run into the limit; 0xffffffff (the default) switches the hook off.  The
- * kernels of qm_linear_int8 and qm_gated_linear_int8 go by both (k-blocks of 128 codes) and leave NaN in the outputs that
+ * kernels of qm_linear_int8, qm_gated_linear_int8 and qm_linear_fp8 go by both (k-blocks of 128 codes) and leave NaN in the outputs that
  * they could not compute.  Both are process-wide and meant for tests only.
  */
 void qm_debug_set_wait_limit_ns(uint64_t ns);
