@@ -16,8 +16,8 @@
 // attention_tiles, for sequences with many query rows: 128 or 256 of them to a thread block. Tiles of 32 keys and values are turned into fp16
 // in shared memory once for all of its warps, the next tile's codes on their way meanwhile.
 //
-// 64 sequences of up to 8192 tokens, 32 heads on 8 of 128: 151 us, 3.6 TB/s of codes; instructions (conversions, products, softmax) bound it, not HBM. 2048 tokens on
-// 4096, the same heads: 480 us, 215 TFLOP/s of the 592 that mma.sync has here (8 cycles a product and scheduler); two warps a scheduler leave its latencies open.
+// 64 sequences of up to 8192 tokens, 32 heads on 8 of 128: 149 us, 3.7 TB/s of codes; instructions (conversions, products, softmax) bound it, not HBM. 2048 tokens on
+// 4096, the same heads: 474 us, 218 TFLOP/s of the 592 that mma.sync has here (8 cycles a product and scheduler); two warps a scheduler leave its latencies open.
 #include <algorithm>
 #include <atomic>
 

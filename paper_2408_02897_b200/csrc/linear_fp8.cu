@@ -6,9 +6,9 @@
 //                     of a cluster, whose sums are added in the order of the parts.
 //   linear_fp8_many   CTA pairs (cta_group::2) on tiles of 256 rows of x and 256 weight rows, two blocks' sums in tensor memory.
 //
-// What the scales cost: 128 entries of a 256 x 256 tile take the CTA pair 680 ns (16384 x 4096 x 1024 92 to 103 us), 505 with the sums left unread. The multiply-adds
+// What the scales cost: 128 entries of a 256 x 256 tile take the CTA pair 610 to 720 ns (16384 x 4096 x 1024 90 to 97 us, 102 to 112 with a bias), 505 with the sums left unread. The multiply-adds
 // are 257 cycles of it, under the MMAs; a buffer's round (MMA, commit, sums to registers, arrival at the leader, next MMA) is longer than two MMA times, and two
-// buffers are all of tensor memory. A scale per weight row too is a second multiplication: 995 ns.
+// buffers are all of tensor memory. A scale per weight row too is a second multiplication: 1000 to 1300 ns.
 //
 // Every mbarrier wait is bounded (Waiter): a CTA that gives up leaves NaN in the outputs it cannot compute, waits for what it has
 // in flight, frees tensor memory and returns.
@@ -49,8 +49,8 @@ __device__ __forceinline__ void add4(float4& a, const float4& b) { a.x += b.x; a
 // ------------------------------------------------------------------ few rows
 // One tile of 128 weight rows x NT rows of x per CTA, or per cluster that splits the contraction.  Roles: warp 0 issues TMA loads into a
 // ring, warp 1 holds tensor memory and issues the MMAs, warps 2..9 add the blocks' sums up: the two warps of a lane quarter take half
-// of the NT columns each (of 16, one of them takes all).  1 x 4096 x 1024 3.2 us, a chain of latencies; 64 x 8192 x 8192 19.3, weights from HBM (10.5 for their
-// bytes): 300 to 500 ns for each 128 entries, 15.7 us with the sums left unread.
+// of the NT columns each (of 16, one of them takes all).  1 x 4096 x 1024 3.2 us, a chain of latencies; 64 x 8192 x 8192 19.2, weights from HBM (10.5 for their
+// bytes): 300 to 550 ns for each 128 entries, 15.7 us with the sums left unread.
 struct FewArgs {
   int64_t M, N;
   int num_kb, tiles_m, split, stages;
