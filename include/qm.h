@@ -422,7 +422,7 @@ qm_status qm_cache_append(const qm_cache* cache, const void* k, int64_t ld_k, co
 /*
  * qm_cache_attention: out = softmax(scale * q . k^T) . v for the new tokens, each over the keys up to and with its own position.
  *  q        bf16 [tokens][heads][head_dim], tokens ld_q elements apart; query head h reads cached head h / (heads / kv_heads)
- *  out      bf16, the same shape, ld_out apart;  q and out 16-byte aligned, ld_* multiples of 8
+ *  out      bf16, the same shape, ld_out apart, no part of it q's;  q and out 16-byte aligned, ld_* multiples of 8
  *  lse      optional (NULL) fp32 [tokens][heads]: log sum exp(scale * q . k), natural
  *  ws       device scratch of at least qm_cache_attention_workspace_bytes(head_dim) bytes, 256-byte aligned; its contents do not matter and
  *           concurrent calls must not share it (nor two captured graphs that may run at the same time)

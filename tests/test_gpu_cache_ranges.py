@@ -1,7 +1,9 @@
 """qm_cache_attention where the scales of a cache lie at the ends of their range, or far apart."""
 import numpy as np
 import pytest
+import torch
 
+import paper_2408_02897_b200 as qm
 from oracle import blocks
 from test_gpu_cache import U, Case, attention_tolerance, run_attention
 
@@ -73,6 +75,35 @@ def test_scales_of_keys_below_the_least_count_as_zero(kv, group, dim, block, new
     top = {"int8": 127.0, "e5m2": 57344.0}[fmt]
     case.dk[held] = np.exp2(case.rng.choice([-62.0, -60.5, -60.0, -59.5], case.dk.shape))[held].astype(np.float32)
     check(case, kv * group, q_scale=2.0 ** 61 / top, scale=2 * dim ** -0.5)
+
+
+@pytest.mark.parametrize("kv,group,dim,block,new,lens", SHAPES)
+def test_rows_done_again_are_the_same_captured_on_another_stream_and_beside_others(kv, group, dim, block, new, lens):
+    """The same bits every time, without the log-sum-exp, into wider rows; rows of sequences whose scales are small keep theirs."""
+    case = Case("int8", kv, dim, block, new, lens, seed=8).fill(lens)
+    q, qd = case.queries(kv * group)
+    ordinary, _ = qm.qm_cache_attention(qd, **case.device())
+    case.dv[case.tables[0, :-(-lens[0] // block)]] *= np.float32(2.0 ** 100)
+    d = case.device()
+    first, lse = qm.qm_cache_attention(qd, **d, want_lse=True)
+    rest = slice(new[0], None)
+    assert torch.isfinite(first).all() and first[:new[0]].abs().max() > 1e20
+    off = (first[rest].float() - ordinary[rest].float()).abs()          # (one of these may share its thread block: two roundings, and the weights' 11 bits)
+    most = max(float(np.nanmax(case.dv[case.tables[b, :-(-n // block)]])) for b, n in enumerate(lens) if b) * 127
+    assert (off <= 2.0 ** -7 * 1.01 * ordinary[rest].float().abs() + 4 * 2.0 ** -11 * most).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = qm.qm_cache_attention(qd, **d, want_lse=True, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(first, other[0]) and torch.equal(lse, other[1])
+    wide = torch.full((case.tokens, kv * group + 2, dim), 5.0, dtype=torch.bfloat16, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        qm.qm_cache_attention(qd, **d, out=wide[:, 1:-1])
+    for _ in range(2):
+        wide[:, 1:-1] = 0.0
+        graph.replay()
+        assert torch.equal(wide[:, 1:-1], first) and (wide[:, 0] == 5.0).all() and (wide[:, -1] == 5.0).all()
 
 
 def test_oracle_counts_least_scales_as_zero():
